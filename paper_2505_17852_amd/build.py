@@ -13,7 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libzo.so")
 OBJ = os.path.join(HERE, "_build")
-SOURCES = ["zo_api.hip", "zo_profile.hip", "k_rng.hip", "k_forward.hip", "k_forward_f32.hip", "k_forward_bf16.hip"]
+SOURCES = ["zo_api.hip", "zo_profile.hip", "k_rng.hip", "k_forward.hip", "k_forward_f32.hip", "k_forward_bf16.hip",
+           "zo_layers.hip", "k_norm.hip", "k_adamw.hip", "k_linattn.hip", "k_linattn_step.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # phase ranges for marker tracing (rocprofiler-sdk's roctx)

@@ -1,0 +1,361 @@
+// Layer norm, forward and backward, over rows of D values.
+//
+// forward   mean and variance of the row (two passes over values held in
+//           registers: the variance is of x - mean, so a large mean costs no
+//           precision), y = (x - mean) rstd w + b
+// backward  g = dy w, xhat = (x - mean) rstd,
+//           dx = rstd (g - avg(g) - xhat avg(g xhat)),
+//           dw = sum dy xhat, db = sum dy over the rows
+//
+// Both are bound by memory: each input is read once and each output written
+// once. A row belongs to 64 or 256 threads, the fewest that hold it in 16
+// registers each (a wave exchanges its sums without a barrier; more threads
+// leave fewer loads per thread in flight), or to 1,024 threads with 8 each (16
+// do not fit the registers of so many). Rows beyond 8,192 values are read again
+// for every pass (the loop kernels).
+//
+// The weight's gradients: a workgroup of the backward pass walks over many rows
+// and keeps its threads' columns' sums in registers; the workgroups' sums go to
+// the workspace, and a second launch adds them, in workgroup order: the same
+// bits every time, no atomics.
+#include <hip/hip_runtime.h>
+
+#include "zo_layers.hpp"
+
+namespace zo {
+namespace {
+
+constexpr int kMaxParts = 512;  // workgroups of a backward pass
+constexpr int kLoopThreads = 1024;
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+  return x;
+}
+
+// Sums of N values over the TPR threads of a row; `buf` alternates between two
+// arrays of a wave's sums, so that one barrier per call is enough.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], float (*buf)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+  if constexpr (TPR > 64) {
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) buf[w][i] = s[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      s[i] = 0;
+#pragma unroll
+      for (int k = 0; k < TPR / 64; ++k) s[i] += buf[k][i];
+    }
+  }
+}
+
+// Values of a row per thread.
+template <int TPR>
+constexpr int vals_of() { return TPR > 256 ? 8 : 16; }
+
+// A thread's values of a row: runs of VEC at (c TPR + lane) VEC.
+template <typename T>
+constexpr int vec_of() { return sizeof(T) == 2 ? 8 : 4; }
+
+template <typename T, int TPR, int VEC>
+__device__ __forceinline__ void load_row(const T* p, int lane, int D, float* out, float fill) {
+  constexpr int kVals = vals_of<TPR>();
+#pragma unroll
+  for (int c = 0; c < kVals / VEC; ++c) {
+    const int j = (c * TPR + lane) * VEC;
+    if (j + VEC <= D) {
+      load_run<T, VEC>(p + j, out + c * VEC);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) out[c * VEC + e] = j + e < D ? to_f32(p[j + e]) : fill;
+    }
+  }
+}
+template <typename T, int TPR, int VEC>
+__device__ __forceinline__ void store_row(T* p, int lane, int D, const float* in) {
+  constexpr int kVals = vals_of<TPR>();
+#pragma unroll
+  for (int c = 0; c < kVals / VEC; ++c) {
+    const int j = (c * TPR + lane) * VEC;
+    if (j + VEC <= D) {
+      store_run<T, VEC>(p + j, in + c * VEC);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (j + e < D) p[j + e] = from_f32<T>(in[c * VEC + e]);
+    }
+  }
+}
+
+// Rows per workgroup at a time: waves of their own rows where one wave holds a row.
+template <int TPR>
+constexpr int threads_of() { return TPR > 256 ? TPR : 256; }
+template <int TPR>
+constexpr int rows_of() { return threads_of<TPR>() / TPR; }
+
+template <typename T, typename W, int TPR>
+__global__ __launch_bounds__(threads_of<TPR>()) void norm_kernel(NormArgs a) {
+  constexpr int VEC = vec_of<T>(), RPB = rows_of<TPR>(), kVals = vals_of<TPR>();
+  __shared__ float buf[2][TPR / 64][1];
+  const int lane = threadIdx.x % TPR, D = (int)a.D;
+  float w[kVals], b[kVals];
+  bool loaded = false;
+  for (int64_t r = block_id() * RPB + threadIdx.x / TPR; r < a.rows; r += (int64_t)gridDim.x * gridDim.y * RPB) {
+    float x[kVals];
+    load_row<T, TPR, VEC>((const T*)a.x + r * a.xs, lane, D, x, 0.0f);
+    if (!loaded) {
+      loaded = true;
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) {
+        w[i] = 1.0f;
+        b[i] = 0.0f;
+      }
+      if (a.w) load_row<W, TPR, VEC>((const W*)a.w, lane, D, w, 0.0f);
+      if (a.b) load_row<W, TPR, VEC>((const W*)a.b, lane, D, b, 0.0f);
+    }
+    float s[1] = {0};
+#pragma unroll
+    for (int i = 0; i < kVals; ++i) s[0] += x[i];
+    row_sums<TPR, 1>(s, buf[0]);
+    const float mean = s[0] / (float)D;
+    s[0] = 0;
+#pragma unroll
+    for (int c = 0; c < kVals / VEC; ++c)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        float& v = x[c * VEC + e];
+        v = (c * TPR + lane) * VEC + e < D ? v - mean : 0.0f;
+        s[0] += v * v;
+      }
+    row_sums<TPR, 1>(s, buf[1]);
+    const float rstd = 1.0f / sqrtf(s[0] / (float)D + a.eps);
+#pragma unroll
+    for (int i = 0; i < kVals; ++i) x[i] = x[i] * rstd * w[i] + b[i];
+    store_row<T, TPR, VEC>((T*)a.y + r * a.ys, lane, D, x);
+    if (a.mean && lane == 0) {
+      a.mean[r] = mean;
+      a.rstd[r] = rstd;
+    }
+  }
+}
+
+template <typename T, typename W, int TPR>
+__global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormArgs a) {
+  constexpr int VEC = vec_of<T>(), RPB = rows_of<TPR>(), NT = threads_of<TPR>(), kVals = vals_of<TPR>();
+  __shared__ float buf[2][TPR / 64][2];
+  __shared__ float join[RPB > 1 ? kVals * NT : 1];
+  const int lane = threadIdx.x % TPR, D = (int)a.D;
+  float w[kVals], dw[kVals], db[kVals];
+#pragma unroll
+  for (int i = 0; i < kVals; ++i) {
+    w[i] = 1.0f;
+    dw[i] = 0.0f;
+    db[i] = 0.0f;
+  }
+  if (a.w) load_row<W, TPR, VEC>((const W*)a.w, lane, D, w, 0.0f);
+  int turn = 0;
+  for (int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; r < a.rows; r += (int64_t)gridDim.x * RPB) {
+    float x[kVals], dy[kVals];
+    load_row<T, TPR, VEC>((const T*)a.x + r * a.xs, lane, D, x, 0.0f);
+    load_row<T, TPR, VEC>((const T*)a.dy + r * a.dys, lane, D, dy, 0.0f);
+    const float mean = a.mean[r], rstd = a.rstd[r];
+    float s[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kVals; ++i) {
+      x[i] = (x[i] - mean) * rstd;  // past the row's end dy is zero, and x never stored
+      db[i] += dy[i];
+      dw[i] += dy[i] * x[i];
+      dy[i] *= w[i];
+      s[0] += dy[i];
+      s[1] += dy[i] * x[i];
+    }
+    row_sums<TPR, 2>(s, buf[turn]);
+    turn ^= 1;
+    const float m0 = s[0] / (float)D, m1 = s[1] / (float)D;
+#pragma unroll
+    for (int i = 0; i < kVals; ++i) x[i] = rstd * (dy[i] - m0 - x[i] * m1);
+    store_row<T, TPR, VEC>((T*)a.y + r * a.ys, lane, D, x);
+  }
+  if (!a.partial) return;
+  // the workgroup's sums: [workgroup][dw, db][D]
+  float* part = a.partial + (int64_t)blockIdx.x * 2 * D;
+  if constexpr (RPB > 1) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kVals; ++i) join[i * NT + threadIdx.x] = q ? db[i] : dw[i];
+      __syncthreads();
+      if (threadIdx.x < TPR)
+#pragma unroll
+        for (int i = 0; i < kVals; ++i) {
+          float& v = q ? db[i] : dw[i];
+          v = 0;
+#pragma unroll
+          for (int k = 0; k < RPB; ++k) v += join[i * NT + k * TPR + threadIdx.x];
+        }
+    }
+    if (threadIdx.x >= TPR) return;
+  }
+  store_row<float, TPR, VEC>(part, lane, D, dw);
+  store_row<float, TPR, VEC>(part + D, lane, D, db);
+}
+
+// Adds the workgroups' sums: 64 columns by 4 shares of the workgroups, then the shares.
+__global__ __launch_bounds__(256) void norm_sums_kernel(const float* partial, int parts, int64_t D, float* dw,
+                                                        float* db) {
+  __shared__ float join[4][64];
+  float* out = blockIdx.y ? db : dw;
+  if (!out) return;
+  const int64_t j = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  const int share = threadIdx.x >> 6;
+  float s = 0;
+  if (j < D) {
+    const float* p = partial + blockIdx.y * D + j;
+#pragma unroll 8
+    for (int k = share; k < parts; k += 4) s += p[(int64_t)k * 2 * D];
+  }
+  join[share][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (share == 0 && j < D) out[j] = (join[0][threadIdx.x] + join[1][threadIdx.x]) + (join[2][threadIdx.x] + join[3][threadIdx.x]);
+}
+
+// Rows of any length: a workgroup per row, every pass reads the row again.
+template <typename T, typename W>
+__global__ __launch_bounds__(kLoopThreads) void norm_loop_kernel(NormArgs a) {
+  __shared__ float buf[2][kLoopThreads / 64][1];
+  for (int64_t r = block_id(); r < a.rows; r += (int64_t)gridDim.x * gridDim.y) {
+    const T* x = (const T*)a.x + r * a.xs;
+    float s[1] = {0};
+    for (int64_t j = threadIdx.x; j < a.D; j += kLoopThreads) s[0] += to_f32(x[j]);
+    row_sums<kLoopThreads, 1>(s, buf[0]);
+    const float mean = s[0] / (float)a.D;
+    s[0] = 0;
+    for (int64_t j = threadIdx.x; j < a.D; j += kLoopThreads) {
+      const float v = to_f32(x[j]) - mean;
+      s[0] += v * v;
+    }
+    row_sums<kLoopThreads, 1>(s, buf[1]);
+    const float rstd = 1.0f / sqrtf(s[0] / (float)a.D + a.eps);
+    T* y = (T*)a.y + r * a.ys;
+    for (int64_t j = threadIdx.x; j < a.D; j += kLoopThreads) {
+      const float w = a.w ? to_f32(((const W*)a.w)[j]) : 1.0f, b = a.b ? to_f32(((const W*)a.b)[j]) : 0.0f;
+      y[j] = from_f32<T>((to_f32(x[j]) - mean) * rstd * w + b);
+    }
+    if (a.mean && threadIdx.x == 0) {
+      a.mean[r] = mean;
+      a.rstd[r] = rstd;
+    }
+  }
+}
+template <typename T, typename W>
+__global__ __launch_bounds__(kLoopThreads) void norm_backward_loop_kernel(NormArgs a) {
+  __shared__ float buf[2][kLoopThreads / 64][2];
+  int turn = 0;
+  for (int64_t r = block_id(); r < a.rows; r += (int64_t)gridDim.x * gridDim.y) {
+    const T *x = (const T*)a.x + r * a.xs, *dy = (const T*)a.dy + r * a.dys;
+    const float mean = a.mean[r], rstd = a.rstd[r];
+    float s[2] = {0, 0};
+    for (int64_t j = threadIdx.x; j < a.D; j += kLoopThreads) {
+      const float g = to_f32(dy[j]) * (a.w ? to_f32(((const W*)a.w)[j]) : 1.0f);
+      s[0] += g;
+      s[1] += g * ((to_f32(x[j]) - mean) * rstd);
+    }
+    row_sums<kLoopThreads, 2>(s, buf[turn]);
+    turn ^= 1;
+    const float m0 = s[0] / (float)a.D, m1 = s[1] / (float)a.D;
+    T* dx = (T*)a.y + r * a.ys;
+    for (int64_t j = threadIdx.x; j < a.D; j += kLoopThreads) {
+      const float g = to_f32(dy[j]) * (a.w ? to_f32(((const W*)a.w)[j]) : 1.0f);
+      dx[j] = from_f32<T>(rstd * (g - m0 - (to_f32(x[j]) - mean) * rstd * m1));
+    }
+  }
+}
+// Column sums of long rows, before dx is written (it may replace dy or x): a
+// thread per column and share of the rows.
+template <typename T>
+__global__ __launch_bounds__(256) void norm_columns_kernel(NormArgs a, int parts) {
+  const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (j >= a.D) return;
+  float dw = 0, db = 0;
+  for (int64_t r = blockIdx.y; r < a.rows; r += parts) {
+    const float g = to_f32(((const T*)a.dy)[r * a.dys + j]);
+    db += g;
+    dw += g * ((to_f32(((const T*)a.x)[r * a.xs + j]) - a.mean[r]) * a.rstd[r]);
+  }
+  float* part = a.partial + (int64_t)blockIdx.y * 2 * a.D;
+  part[j] = dw;
+  part[a.D + j] = db;
+}
+
+int row_threads(int64_t D) { return D <= 1024 ? 64 : D <= 4096 ? 256 : D <= 8192 ? 1024 : 0; }
+
+// Workgroups of a backward pass, each with sums of its own.
+int parts_of(int64_t rows, int64_t D) {
+  const int tpr = row_threads(D);
+  const int64_t need = tpr == 64 ? (rows + 3) / 4 : rows;
+  return (int)(need < kMaxParts ? need : kMaxParts);
+}
+
+template <typename T, typename W>
+hipError_t forward(const NormArgs& a, hipStream_t s) {
+  const int tpr = row_threads(a.D);
+  const dim3 grid = wide_grid(tpr == 64 ? (a.rows + 3) / 4 : a.rows);
+  if (tpr == 64) norm_kernel<T, W, 64><<<grid, 256, 0, s>>>(a);
+  else if (tpr == 256) norm_kernel<T, W, 256><<<grid, 256, 0, s>>>(a);
+  else if (tpr == 1024) norm_kernel<T, W, 1024><<<grid, 1024, 0, s>>>(a);
+  else norm_loop_kernel<T, W><<<grid, kLoopThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, typename W>
+hipError_t backward(const NormArgs& a, hipStream_t s) {
+  const int parts = parts_of(a.rows, a.D), tpr = row_threads(a.D);
+  if (a.rows) {
+    if (tpr == 64) norm_backward_kernel<T, W, 64><<<parts, 256, 0, s>>>(a);
+    else if (tpr == 256) norm_backward_kernel<T, W, 256><<<parts, 256, 0, s>>>(a);
+    else if (tpr == 1024) norm_backward_kernel<T, W, 1024><<<parts, 1024, 0, s>>>(a);
+    else {
+      if (a.partial)
+        norm_columns_kernel<T><<<dim3((unsigned)((a.D + 255) / 256), parts), 256, 0, s>>>(a, parts);
+      norm_backward_loop_kernel<T, W><<<wide_grid(a.rows), kLoopThreads, 0, s>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.dw || a.db)
+    norm_sums_kernel<<<dim3((unsigned)((a.D + 63) / 64), 2), 256, 0, s>>>(a.partial, parts, a.D, a.dw, a.db);
+  return hipGetLastError();
+}
+
+template <typename F>
+hipError_t by_type(const NormArgs& a, F f) {
+  const bool xb = a.xdtype == ZO_WBF16, wb = a.wdtype == ZO_WBF16;
+  if (xb) return wb ? f((uint16_t*)nullptr, (uint16_t*)nullptr) : f((uint16_t*)nullptr, (float*)nullptr);
+  return wb ? f((float*)nullptr, (uint16_t*)nullptr) : f((float*)nullptr, (float*)nullptr);
+}
+
+}  // namespace
+
+size_t norm_workspace(int64_t rows, int64_t D) { return (size_t)parts_of(rows, D) * 2 * (size_t)D * sizeof(float); }
+
+hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
+  if (a.rows == 0) return hipSuccess;
+  return by_type(a, [&](auto t, auto w) {
+    return forward<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(w)>>(a, s);
+  });
+}
+
+hipError_t launch_norm_backward(const NormArgs& a, hipStream_t s) {
+  return by_type(a, [&](auto t, auto w) {
+    return backward<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(w)>>(a, s);
+  });
+}
+
+}  // namespace zo

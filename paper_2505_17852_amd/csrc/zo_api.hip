@@ -4,38 +4,20 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <mutex>
 
 #include "../../include/zo.h"
 #include "zo_common.hpp"
+#include "zo_error.hpp"
 #include "zo_kernels.hpp"
 #include "zo_profile.hpp"
 
 namespace {
 
-thread_local char g_err[512] = "";
-
-int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-int fail(int code, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  std::vsnprintf(g_err, sizeof g_err, fmt, ap);
-  va_end(ap);
-  return code;
-}
-
-int ok() {
-  g_err[0] = '\0';
-  return ZO_OK;
-}
-
-int device_status(hipError_t e, const char* what) {
-  if (e == hipSuccess) return ok();
-  return fail(ZO_EDEVICE, "%s: %s", what, hipGetErrorString(e));
-}
+using zo::aligned16;
+using zo::device_status;
+using zo::fail;
 
 // Shape rules of the kernels: every matrix dimension that a K tile or a
 // column tile walks is a multiple of 32 (so that a 32-element probe word
@@ -47,8 +29,6 @@ int check_config(const zo_config* c) {
                 c->hidden);
   return ZO_OK;
 }
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 // Workspace of zo_perturbed_losses_noalloc: a fixed device array, one copy per
 // device, held until the process ends, half as large again as the account
@@ -316,6 +296,6 @@ int zo_debug_gauss_pairs(const uint32_t* words, uint64_t n_pairs, float* out, vo
                        "zo_debug_gauss_pairs");
 }
 
-const char* zo_last_error(void) { return g_err; }
+const char* zo_last_error(void) { return zo::g_err; }
 
 }  // extern "C"

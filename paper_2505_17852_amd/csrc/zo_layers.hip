@@ -1,0 +1,369 @@
+// C ABI entry points of the layers (zo_layers.h): argument validation on the
+// host, then kernel launches on the caller's stream. Nothing here allocates
+// device memory.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "zo_error.hpp"
+#include "zo_layers.hpp"
+#include "zo_profile.hpp"
+
+namespace {
+
+using zo::aligned16;
+using zo::device_status;
+using zo::fail;
+using zo::ok;
+
+bool is_type(int32_t t) { return t == ZO_WFP32 || t == ZO_WBF16; }
+size_t type_bytes(int32_t t) { return t == ZO_WBF16 ? 2 : 4; }
+bool aligned_for(const void* p, int32_t t) { return ((uintptr_t)p & (type_bytes(t) - 1)) == 0; }
+bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
+int check_linattn(const zo_linattn* s) {
+  if (!s) return fail(ZO_EINVAL, "shape is NULL");
+  if (s->batch < 0 || s->length < 0) return fail(ZO_EINVAL, "batch and length must be >= 0");
+  if (s->q_heads < 1 || s->kv_heads < 1 || s->q_heads % s->kv_heads)
+    return fail(ZO_EINVAL, "q_heads (%d) must be a positive multiple of kv_heads (%d)", s->q_heads, s->kv_heads);
+  if (s->key_dim < 1 || s->value_dim < 1) return fail(ZO_EINVAL, "key_dim and value_dim must be >= 1");
+  if (s->key_dim > ZO_LINATTN_MAX_DIM || s->value_dim > ZO_LINATTN_MAX_DIM)
+    return fail(ZO_ESHAPE, "key_dim (%d) and value_dim (%d) must be <= %d", s->key_dim, s->value_dim,
+                ZO_LINATTN_MAX_DIM);
+  if (!is_type(s->dtype)) return fail(ZO_EINVAL, "unknown dtype %d", s->dtype);
+  if (!std::isfinite(s->scale)) return fail(ZO_EINVAL, "scale must be finite");
+  if ((int64_t)s->batch * s->q_heads > (int64_t)1 << 31) return fail(ZO_ESHAPE, "batch * q_heads too many");
+  return ZO_OK;
+}
+
+// A tensor that is read or written (its elements exist when `any`).
+int check_heads(const zo_heads* h, const char* name, int32_t dtype, bool any) {
+  if (!h) return fail(ZO_EINVAL, "%s is NULL", name);
+  if (any && !h->data) return fail(ZO_EINVAL, "%s has no data", name);
+  if (!aligned_for(h->data, dtype)) return fail(ZO_EINVAL, "%s is not aligned to its type", name);
+  return ZO_OK;
+}
+
+zo::Heads heads(const zo_heads* h) {
+  return zo::Heads{h->data, h->batch_stride, h->position_stride, h->head_stride};
+}
+
+int check_state(const float* s, const char* name) {
+  return aligned4(s) ? ZO_OK : fail(ZO_EINVAL, "%s is not aligned to its type", name);
+}
+
+int check_workspace(const zo_linattn* s, bool backward, const void* workspace, size_t bytes) {
+  const size_t need = zo::linattn_workspace(*s, backward);
+  if (bytes < need) return fail(ZO_ENOMEM, "workspace of %zu bytes < %zu required", bytes, need);
+  if (need && !workspace) return fail(ZO_EINVAL, "workspace is NULL");
+  if (!aligned16(workspace)) return fail(ZO_EINVAL, "workspace must be 16-byte aligned");
+  return ZO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t zo_linear_attention_workspace_bytes(const zo_linattn* shape, int32_t backward) {
+  if (check_linattn(shape)) return 0;
+  return zo::linattn_workspace(*shape, backward != 0);
+}
+
+int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_heads* k, const zo_heads* v,
+                        const zo_heads* o, const float* log_decay, const int32_t* lengths,
+                        const float* initial_state, float* final_state, void* workspace, size_t ws_bytes,
+                        void* stream) {
+  zo::PhaseRange range("zo_linear_attention");
+  int st = check_linattn(shape);
+  if (st) return st;
+  const zo_linattn& s = *shape;
+  const bool any = s.batch > 0 && s.length > 0;
+  if ((st = check_heads(q, "q", s.dtype, any)) || (st = check_heads(k, "k", s.dtype, any)) ||
+      (st = check_heads(v, "v", s.dtype, any)) || (st = check_heads(o, "o", s.dtype, any)) ||
+      (st = check_state(log_decay, "log_decay")) || (st = check_state(initial_state, "initial_state")) ||
+      (st = check_state(final_state, "final_state")) || (st = check_workspace(shape, false, workspace, ws_bytes)))
+    return st;
+  if (!log_decay) return fail(ZO_EINVAL, "log_decay is NULL");
+  if (((uintptr_t)lengths & 3u) != 0) return fail(ZO_EINVAL, "lengths is not aligned to its type");
+  zo::LinCall c{};
+  zo::LinPass& p = c.pass[0];
+  p.x = heads(q);
+  p.y = heads(k);
+  p.z = heads(v);
+  p.out = o->data;
+  p.ob = o->batch_stride;
+  p.ot = o->position_stride;
+  p.oh = o->head_stride;
+  p.dx = s.key_dim;
+  p.dz = s.value_dim;
+  p.out_heads = s.q_heads;
+  p.sources = 1;
+  p.share = s.q_heads / s.kv_heads;
+  p.score = p.carry = s.scale;
+  p.upd = 1.0f;
+  p.init = initial_state;
+  p.fin = final_state;
+  c.npasses = 1;
+  c.B = s.batch;
+  c.T = s.length;
+  c.kv_heads = s.kv_heads;
+  c.dtype = s.dtype;
+  c.log_decay = log_decay;
+  c.lengths = lengths;
+  c.work = workspace;
+  return device_status(zo::launch_linattn(c, (hipStream_t)stream), "zo_linear_attention");
+}
+
+int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, const zo_heads* q,
+                                 const zo_heads* k, const zo_heads* v, const zo_heads* dq, const zo_heads* dk,
+                                 const zo_heads* dv, const float* log_decay, const int32_t* lengths,
+                                 const float* initial_state, const float* dfinal_state, float* dinitial_state,
+                                 void* workspace, size_t ws_bytes, void* stream) {
+  zo::PhaseRange range("zo_linear_attention_backward");
+  int st = check_linattn(shape);
+  if (st) return st;
+  const zo_linattn& s = *shape;
+  const bool any = s.batch > 0 && s.length > 0;
+  if ((st = check_heads(dout, "dout", s.dtype, any)) || (st = check_heads(q, "q", s.dtype, any)) ||
+      (st = check_heads(k, "k", s.dtype, any)) || (st = check_heads(v, "v", s.dtype, any)) ||
+      (st = check_heads(dq, "dq", s.dtype, any)) || (st = check_heads(dk, "dk", s.dtype, any)) ||
+      (st = check_heads(dv, "dv", s.dtype, any)) || (st = check_state(log_decay, "log_decay")) ||
+      (st = check_state(initial_state, "initial_state")) || (st = check_state(dfinal_state, "dfinal_state")) ||
+      (st = check_state(dinitial_state, "dinitial_state")) ||
+      (st = check_workspace(shape, true, workspace, ws_bytes)))
+    return st;
+  if (!log_decay) return fail(ZO_EINVAL, "log_decay is NULL");
+  if (((uintptr_t)lengths & 3u) != 0) return fail(ZO_EINVAL, "lengths is not aligned to its type");
+  const int share = s.q_heads / s.kv_heads;
+  zo::LinCall c{};
+  // dq: forward in time, the transposed state
+  zo::LinPass& a = c.pass[0];
+  a.x = heads(dout);
+  a.y = heads(v);
+  a.z = heads(k);
+  a.out = dq->data;
+  a.ob = dq->batch_stride;
+  a.ot = dq->position_stride;
+  a.oh = dq->head_stride;
+  a.dx = s.value_dim;
+  a.dz = s.key_dim;
+  a.out_heads = s.q_heads;
+  a.sources = 1;
+  a.share = share;
+  a.state_t = 1;
+  a.score = a.carry = s.scale;
+  a.upd = 1.0f;
+  a.init = initial_state;
+  // dv: backward in time, the gradient of the state
+  zo::LinPass& d = c.pass[1];
+  d.x = heads(k);
+  d.y = heads(q);
+  d.z = heads(dout);
+  d.out = dv->data;
+  d.ob = dv->batch_stride;
+  d.ot = dv->position_stride;
+  d.oh = dv->head_stride;
+  d.dx = s.key_dim;
+  d.dz = s.value_dim;
+  d.out_heads = s.kv_heads;
+  d.sources = share;
+  d.share = 1;
+  d.reverse = 1;
+  d.score = d.upd = s.scale;
+  d.carry = 1.0f;
+  d.init = dfinal_state;
+  d.fin = dinitial_state;
+  // dk: backward in time, its transpose
+  zo::LinPass& e = c.pass[2];
+  e = d;
+  e.x = heads(v);
+  e.y = heads(dout);
+  e.z = heads(q);
+  e.out = dk->data;
+  e.ob = dk->batch_stride;
+  e.ot = dk->position_stride;
+  e.oh = dk->head_stride;
+  e.dx = s.value_dim;
+  e.dz = s.key_dim;
+  e.state_t = 1;
+  e.fin = nullptr;
+  c.npasses = 3;
+  c.B = s.batch;
+  c.T = s.length;
+  c.kv_heads = s.kv_heads;
+  c.dtype = s.dtype;
+  c.log_decay = log_decay;
+  c.lengths = lengths;
+  c.work = workspace;
+  return device_status(zo::launch_linattn(c, (hipStream_t)stream), "zo_linear_attention_backward");
+}
+
+int zo_linear_attention_step(const zo_linattn* shape, const zo_heads* q, const zo_heads* k, const zo_heads* v,
+                             const zo_heads* o, const float* log_decay, float* state, int32_t n_slots,
+                             const int32_t* slots, void* stream) {
+  zo::PhaseRange range("zo_linear_attention_step");
+  int st = check_linattn(shape);
+  if (st) return st;
+  const zo_linattn& s = *shape;
+  const bool any = s.batch > 0;
+  if ((st = check_heads(q, "q", s.dtype, any)) || (st = check_heads(k, "k", s.dtype, any)) ||
+      (st = check_heads(v, "v", s.dtype, any)) || (st = check_heads(o, "o", s.dtype, any)) ||
+      (st = check_state(log_decay, "log_decay")) || (st = check_state(state, "state")))
+    return st;
+  if (!log_decay || (!state && n_slots > 0)) return fail(ZO_EINVAL, "a required pointer is NULL");
+  if (n_slots < 0 || (!slots && n_slots < s.batch))
+    return fail(ZO_EINVAL, "n_slots (%d) must be >= 0, and >= batch (%d) without slots", n_slots, s.batch);
+  if (((uintptr_t)slots & 3u) != 0) return fail(ZO_EINVAL, "slots is not aligned to its type");
+  zo::LinStep a{};
+  a.q = heads(q);
+  a.k = heads(k);
+  a.v = heads(v);
+  a.o = o->data;
+  a.ob = o->batch_stride;
+  a.oh = o->head_stride;
+  a.B = s.batch;
+  a.q_heads = s.q_heads;
+  a.kv_heads = s.kv_heads;
+  a.dk = s.key_dim;
+  a.dv = s.value_dim;
+  a.dtype = s.dtype;
+  a.scale = s.scale;
+  a.log_decay = log_decay;
+  a.state = state;
+  a.n_slots = n_slots;
+  a.slots = slots;
+  return device_status(zo::launch_linattn_step(a, (hipStream_t)stream), "zo_linear_attention_step");
+}
+
+static int check_norm(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t D) {
+  if (!is_type(xdtype) || !is_type(wdtype)) return fail(ZO_EINVAL, "unknown dtype (%d, %d)", xdtype, wdtype);
+  if (rows < 0 || D < 1) return fail(ZO_EINVAL, "rows must be >= 0 and D >= 1");
+  if (D > (int64_t)1 << 30) return fail(ZO_ESHAPE, "D must be <= 2^30");
+  if (rows > (int64_t)1 << 36) return fail(ZO_ESHAPE, "rows must be <= 2^36");
+  return ZO_OK;
+}
+
+int zo_layer_norm(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t D, const void* x, int64_t x_stride,
+                  const void* weight, const void* bias, float eps, void* y, int64_t y_stride, float* mean,
+                  float* rstd, void* stream) {
+  zo::PhaseRange range("zo_layer_norm");
+  int st = check_norm(xdtype, wdtype, rows, D);
+  if (st) return st;
+  if (rows > 0 && (!x || !y)) return fail(ZO_EINVAL, "a required pointer is NULL");
+  if (!mean != !rstd) return fail(ZO_EINVAL, "mean and rstd go together");
+  if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(ZO_EINVAL, "eps must be finite and >= 0");
+  if (!aligned_for(x, xdtype) || !aligned_for(y, xdtype) || !aligned_for(weight, wdtype) ||
+      !aligned_for(bias, wdtype) || !aligned4(mean) || !aligned4(rstd))
+    return fail(ZO_EINVAL, "a buffer is not aligned to its type");
+  zo::NormArgs a{};
+  a.xdtype = xdtype;
+  a.wdtype = wdtype;
+  a.rows = rows;
+  a.D = D;
+  a.x = x;
+  a.xs = x_stride;
+  a.w = weight;
+  a.b = bias;
+  a.eps = eps;
+  a.y = y;
+  a.ys = y_stride;
+  a.mean = mean;
+  a.rstd = rstd;
+  return device_status(zo::launch_norm(a, (hipStream_t)stream), "zo_layer_norm");
+}
+
+size_t zo_layer_norm_workspace_bytes(int64_t rows, int64_t D) {
+  return check_norm(ZO_WFP32, ZO_WFP32, rows, D) ? 0 : zo::norm_workspace(rows, D);
+}
+
+int zo_layer_norm_backward(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t D, const void* dy,
+                           int64_t dy_stride, const void* x, int64_t x_stride, const void* weight,
+                           const float* mean, const float* rstd, void* dx, int64_t dx_stride, float* dweight,
+                           float* dbias, void* workspace, size_t ws_bytes, void* stream) {
+  zo::PhaseRange range("zo_layer_norm_backward");
+  int st = check_norm(xdtype, wdtype, rows, D);
+  if (st) return st;
+  if (rows > 0 && (!dy || !x || !mean || !rstd || !dx)) return fail(ZO_EINVAL, "a required pointer is NULL");
+  if (!aligned_for(x, xdtype) || !aligned_for(dy, xdtype) || !aligned_for(dx, xdtype) ||
+      !aligned_for(weight, wdtype) || !aligned4(mean) || !aligned4(rstd) || !aligned4(dweight) || !aligned4(dbias))
+    return fail(ZO_EINVAL, "a buffer is not aligned to its type");
+  const bool sums = dweight || dbias;
+  if (sums) {
+    const size_t need = zo::norm_workspace(rows, D);
+    if (ws_bytes < need) return fail(ZO_ENOMEM, "workspace of %zu bytes < %zu required", ws_bytes, need);
+    if (need && !workspace) return fail(ZO_EINVAL, "workspace is NULL");
+    if (!aligned16(workspace)) return fail(ZO_EINVAL, "workspace must be 16-byte aligned");
+  }
+  zo::NormArgs a{};
+  a.xdtype = xdtype;
+  a.wdtype = wdtype;
+  a.rows = rows;
+  a.D = D;
+  a.x = x;
+  a.xs = x_stride;
+  a.w = weight;
+  a.y = dx;
+  a.ys = dx_stride;
+  a.dy = dy;
+  a.dys = dy_stride;
+  a.mean = const_cast<float*>(mean);
+  a.rstd = const_cast<float*>(rstd);
+  a.dw = dweight;
+  a.db = dbias;
+  a.partial = sums ? (float*)workspace : nullptr;
+  return device_status(zo::launch_norm_backward(a, (hipStream_t)stream), "zo_layer_norm_backward");
+}
+
+int zo_adamw(const zo_adamw_config* cfg, const zo_adamw_tensor* tensors, int32_t n_tensors, void* m, void* v,
+             float* m_scale, float* v_scale, const float* grad_scale, int32_t* skipped_out, void* stream) {
+  zo::PhaseRange range("zo_adamw");
+  if (!cfg) return fail(ZO_EINVAL, "cfg is NULL");
+  if (!std::isfinite(cfg->lr) || !(cfg->eps >= 0.0) || !std::isfinite(cfg->eps))
+    return fail(ZO_EINVAL, "lr must be finite, eps finite and >= 0");
+  if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0))
+    return fail(ZO_EINVAL, "beta1 and beta2 must lie in [0, 1)");
+  if (cfg->step < 1) return fail(ZO_EINVAL, "step must be >= 1");
+  if (cfg->state_bits != 32 && cfg->state_bits != 8) return fail(ZO_EINVAL, "state_bits must be 32 or 8");
+  if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return fail(ZO_EINVAL, "n_tensors < 0, or tensors is NULL");
+  bool any = false;
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const zo_adamw_tensor& t = tensors[i];
+    if (t.n < 0 || t.n > (int64_t)1 << 40) return fail(ZO_EINVAL, "tensor %d: n must lie in [0, 2^40]", i);
+    if (!is_type(t.pdtype) || !is_type(t.gdtype)) return fail(ZO_EINVAL, "tensor %d: unknown dtype", i);
+    if (t.n > 0 && (!t.param || !t.grad)) return fail(ZO_EINVAL, "tensor %d: param or grad is NULL", i);
+    if (!aligned_for(t.param, t.pdtype) || !aligned_for(t.grad, t.gdtype))
+      return fail(ZO_EINVAL, "tensor %d is not aligned to its type", i);
+    if (t.state_offset < 0 || t.state_offset % ZO_ADAMW_BLOCK)
+      return fail(ZO_EINVAL, "tensor %d: state_offset must be a multiple of %d", i, ZO_ADAMW_BLOCK);
+    if (!std::isfinite(t.weight_decay)) return fail(ZO_EINVAL, "tensor %d: weight_decay must be finite", i);
+    any |= t.n > 0;
+  }
+  if (any && (!m || !v)) return fail(ZO_EINVAL, "m or v is NULL");
+  if (!aligned16(m) || !aligned16(v)) return fail(ZO_EINVAL, "m and v must be 16-byte aligned");
+  if (cfg->state_bits == 8) {
+    if (any && (!m_scale || !v_scale)) return fail(ZO_EINVAL, "8-bit moments need m_scale and v_scale");
+  } else if (m_scale || v_scale) {
+    return fail(ZO_EINVAL, "32-bit moments take no m_scale or v_scale");
+  }
+  if (!aligned4(m_scale) || !aligned4(v_scale) || !aligned4(grad_scale) || !aligned4(skipped_out))
+    return fail(ZO_EINVAL, "a buffer is not aligned to its type");
+  return device_status(zo::launch_adamw(*cfg, tensors, n_tensors, m, v, m_scale, v_scale, grad_scale, skipped_out,
+                                        (hipStream_t)stream),
+                       "zo_adamw");
+}
+
+int zo_adamw_moments(int64_t n, const void* m, const void* v, const float* m_scale, const float* v_scale,
+                     float* m_out, float* v_out, void* stream) {
+  zo::PhaseRange range("zo_adamw_moments");
+  if (n < 0 || n % ZO_ADAMW_BLOCK) return fail(ZO_EINVAL, "n must be a multiple of %d", ZO_ADAMW_BLOCK);
+  if (n > (int64_t)1 << 40) return fail(ZO_EINVAL, "n must be <= 2^40");
+  if (n && (!m || !v || !m_scale || !v_scale || !m_out || !v_out))
+    return fail(ZO_EINVAL, "a required pointer is NULL");
+  if (!aligned16(m) || !aligned16(v) || !aligned16(m_out) || !aligned16(v_out) || !aligned4(m_scale) ||
+      !aligned4(v_scale))
+    return fail(ZO_EINVAL, "m, v, m_out and v_out must be 16-byte aligned");
+  return device_status(zo::launch_adamw_moments(n, m, v, m_scale, v_scale, m_out, v_out, (hipStream_t)stream),
+                       "zo_adamw_moments");
+}
+
+}  // extern "C"

@@ -1,0 +1,402 @@
+"""Python binding of the layers of a recurrent language model (include/zo_layers.h):
+linear attention with a decay for each head, layer norm and AdamW.
+
+Argument marshalling only: every computation runs in the library's HIP
+kernels, on the current torch stream unless one is passed. Outputs and
+workspaces are allocated by torch when they are not given. Errors: ValueError
+for arguments that do not fit together, zo.ZoError for what the library refuses.
+
+    layer_norm, layer_norm_backward
+    linear_attention, linear_attention_backward, linear_attention_step
+    AdamW (step, moments)
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import zo
+
+MAX_DIM = 256   # ZO_LINATTN_MAX_DIM
+BLOCK = 256     # ZO_ADAMW_BLOCK
+_DTYPES = {torch.float32: zo.FP32, torch.bfloat16: zo.BF16}
+
+
+class _Shape(C.Structure):  # zo_linattn
+    _fields_ = [(n, C.c_int32) for n in ("batch", "length", "q_heads", "kv_heads", "key_dim", "value_dim", "dtype")]
+    _fields_ += [("scale", C.c_float)]
+
+
+class _Heads(C.Structure):  # zo_heads
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("position_stride", C.c_int64),
+                ("head_stride", C.c_int64)]
+
+
+class _Tensor(C.Structure):  # zo_adamw_tensor
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("n", C.c_int64), ("state_offset", C.c_int64),
+                ("weight_decay", C.c_double), ("pdtype", C.c_int32), ("gdtype", C.c_int32)]
+
+
+class _AdamWConfig(C.Structure):  # zo_adamw_config
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("step", C.c_int64), ("state_bits", C.c_int32)]
+
+
+_lib = None
+
+
+def lib():
+    """The loaded library with the layers' signatures; raises if it has not been built."""
+    global _lib
+    if _lib is None:
+        L = zo.lib()
+        vp, shape, heads, i32, i64 = C.c_void_p, C.POINTER(_Shape), C.POINTER(_Heads), C.c_int32, C.c_int64
+        L.zo_linear_attention_workspace_bytes.argtypes = [shape, i32]
+        L.zo_linear_attention_workspace_bytes.restype = C.c_size_t
+        L.zo_linear_attention.argtypes = [shape] + [heads] * 4 + [vp] * 5 + [C.c_size_t, vp]
+        L.zo_linear_attention_backward.argtypes = [shape] + [heads] * 7 + [vp] * 6 + [C.c_size_t, vp]
+        L.zo_linear_attention_step.argtypes = [shape] + [heads] * 4 + [vp, vp, i32, vp, vp]
+        L.zo_layer_norm.argtypes = [i32, i32, i64, i64, vp, i64, vp, vp, C.c_float, vp, i64, vp, vp, vp]
+        L.zo_layer_norm_workspace_bytes.argtypes = [i64, i64]
+        L.zo_layer_norm_workspace_bytes.restype = C.c_size_t
+        L.zo_layer_norm_backward.argtypes = [i32, i32, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp,
+                                             C.c_size_t, vp]
+        L.zo_adamw.argtypes = [C.POINTER(_AdamWConfig), C.POINTER(_Tensor), i32, vp, vp, vp, vp, vp, vp, vp]
+        L.zo_adamw_moments.argtypes = [i64] + [vp] * 7
+        for f in ("zo_linear_attention", "zo_linear_attention_backward", "zo_linear_attention_step", "zo_layer_norm",
+                  "zo_layer_norm_backward", "zo_adamw", "zo_adamw_moments"):
+            getattr(L, f).restype = C.c_int
+        _lib = L
+    return _lib
+
+
+def _check(st: int):
+    if st:
+        zo._check(st)
+
+
+def _stream(stream):
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _device(t: torch.Tensor, name: str, dtype=None, like: torch.Tensor | None = None):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if dtype is None:
+        if t.dtype not in _DTYPES:
+            raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    elif t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+
+
+def _flat(t: torch.Tensor | None, name: str, dtype, shape, like: torch.Tensor):
+    """The address of a contiguous tensor of a given shape, or None."""
+    if t is None:
+        return None
+    _device(t, name, dtype, like)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _on_stream(stream, *tensors):
+    """Tensors allocated here for a call on another stream than the current one belong to that stream."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+# ---- linear attention ----
+
+def _heads(t: torch.Tensor, name: str, shape, like: torch.Tensor) -> _Heads:
+    if not isinstance(t, torch.Tensor) or t.device != like.device:
+        raise ValueError(f"{name} must be a tensor on {like.device}")
+    if t.dtype != like.dtype:
+        raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] != 1:
+        raise ValueError(f"the values of a head must be contiguous in {name}")
+    return _Heads(t.data_ptr(), st[0], st[1] if len(st) == 4 else 0, st[-2])
+
+
+def _sizes(q, k, v, dims: int, scale):
+    """(shape struct, q's, k's and v's structs) of tensors [B, T, heads, dim], or [B, heads, dim]."""
+    _device(q, "q")
+    if q.dim() != dims or k.dim() != dims or v.dim() != dims:
+        raise ValueError(f"q, k and v must have {dims} dimensions")
+    lead = tuple(q.shape[:-2])
+    Hq, Dk = q.shape[-2:]
+    Hkv, Dv = v.shape[-2:]
+    if Hkv < 1 or Hq % Hkv:
+        raise ValueError(f"{Hq} query heads are no multiple of {Hkv} key/value heads")
+    s = _Shape(lead[0], lead[1] if dims == 4 else 1, Hq, Hkv, Dk, Dv, _DTYPES[q.dtype],
+               Dk ** -0.5 if scale is None else scale)
+    return (s, _heads(q, "q", (*lead, Hq, Dk), q), _heads(k, "k", (*lead, Hkv, Dk), q),
+            _heads(v, "v", (*lead, Hkv, Dv), q))
+
+
+def _workspace(given: torch.Tensor | None, need: int, like: torch.Tensor):
+    """(tensor or None, its address, its bytes)."""
+    if given is None:
+        if need == 0:
+            return None, None, 0
+        given = torch.empty(need, dtype=torch.uint8, device=like.device)
+    else:
+        _device(given, "workspace", torch.uint8, like)
+        if not given.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+    return given, given.data_ptr(), given.numel()
+
+
+def linear_attention_workspace_bytes(B: int, T: int, q_heads: int, kv_heads: int, key_dim: int, value_dim: int,
+                                     dtype=torch.float32, backward: bool = False) -> int:
+    s = _Shape(B, T, q_heads, kv_heads, key_dim, value_dim, _DTYPES[dtype], 1.0)
+    return int(lib().zo_linear_attention_workspace_bytes(C.byref(s), int(backward)))
+
+
+def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                     scale: float | None = None, initial_state: torch.Tensor | None = None,
+                     lengths: torch.Tensor | None = None, return_state: bool = False,
+                     out: torch.Tensor | None = None, final_state: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None, stream=None):
+    """Returns (o, final state or None), asynchronously.
+
+    q [B, T, Hq, Dk], k [B, T, Hkv, Dk], v [B, T, Hkv, Dv] fp32 or bf16, any strides with
+    contiguous heads; log_decay fp32 [Hkv]; scale defaults to Dk ** -0.5; states fp32
+    [B, Hkv, Dk, Dv]; lengths int32 [B] or None (all T). The final state is returned with
+    return_state, or written into final_state (which may be initial_state)."""
+    L = lib()
+    s, hq, hk, hv = _sizes(q, k, v, 4, scale)
+    B, T, Hkv = s.batch, s.length, s.kv_heads
+    states = (B, Hkv, s.key_dim, s.value_dim)
+    o = torch.empty((B, T, s.q_heads, s.value_dim), dtype=q.dtype, device=q.device) if out is None else out
+    if final_state is None and return_state:
+        final_state = torch.empty(states, dtype=torch.float32, device=q.device)
+    f32 = torch.float32
+    ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(C.byref(s), 0), q)
+    _check(L.zo_linear_attention(
+        C.byref(s), C.byref(hq), C.byref(hk), C.byref(hv),
+        C.byref(_heads(o, "out", (B, T, s.q_heads, s.value_dim), q)), _flat(log_decay, "log_decay", f32, (Hkv,), q),
+        _flat(lengths, "lengths", torch.int32, (B,), q), _flat(initial_state, "initial_state", f32, states, q),
+        _flat(final_state, "final_state", f32, states, q), wp, wn, _stream(stream)))
+    _on_stream(stream, o, final_state, ws)
+    return o, final_state
+
+
+def linear_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                              log_decay: torch.Tensor, scale: float | None = None,
+                              initial_state: torch.Tensor | None = None, lengths: torch.Tensor | None = None,
+                              dfinal_state: torch.Tensor | None = None, return_dinitial: bool | None = None,
+                              dq: torch.Tensor | None = None, dk: torch.Tensor | None = None,
+                              dv: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """Returns (dq, dk, dv, dinitial_state or None) for the output's gradient do
+    [B, T, Hq, Dv] and the final state's dfinal_state (None: zeros), asynchronously.
+    The initial state's gradient is computed when one was given, or as return_dinitial says."""
+    L = lib()
+    s, hq, hk, hv = _sizes(q, k, v, 4, scale)
+    B, T, Hq, Hkv, Dk, Dv = s.batch, s.length, s.q_heads, s.kv_heads, s.key_dim, s.value_dim
+    states = (B, Hkv, Dk, Dv)
+    dq = torch.empty((B, T, Hq, Dk), dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty((B, T, Hkv, Dk), dtype=q.dtype, device=q.device) if dk is None else dk
+    dv = torch.empty((B, T, Hkv, Dv), dtype=q.dtype, device=q.device) if dv is None else dv
+    if return_dinitial is None:
+        return_dinitial = initial_state is not None
+    dinitial = torch.empty(states, dtype=torch.float32, device=q.device) if return_dinitial else None
+    f32 = torch.float32
+    ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(C.byref(s), 1), q)
+    _check(L.zo_linear_attention_backward(
+        C.byref(s), C.byref(_heads(do, "do", (B, T, Hq, Dv), q)), C.byref(hq), C.byref(hk), C.byref(hv),
+        C.byref(_heads(dq, "dq", (B, T, Hq, Dk), q)), C.byref(_heads(dk, "dk", (B, T, Hkv, Dk), q)),
+        C.byref(_heads(dv, "dv", (B, T, Hkv, Dv), q)), _flat(log_decay, "log_decay", f32, (Hkv,), q),
+        _flat(lengths, "lengths", torch.int32, (B,), q), _flat(initial_state, "initial_state", f32, states, q),
+        _flat(dfinal_state, "dfinal_state", f32, states, q), _flat(dinitial, "dinitial", f32, states, q), wp, wn,
+        _stream(stream)))
+    _on_stream(stream, dq, dk, dv, dinitial, ws)
+    return dq, dk, dv, dinitial
+
+
+def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                          state: torch.Tensor, scale: float | None = None, slots: torch.Tensor | None = None,
+                          out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """One token for each of B sequences: q [B, Hq, Dk], k [B, Hkv, Dk], v [B, Hkv, Dv] -> o
+    [B, Hq, Dv] (asynchronous); state fp32 [n, Hkv, Dk, Dv] is updated in place. slots (int32
+    [B], no two alike) names each sequence's state in it, -1 a sequence without one (its
+    output is zero); None: sequence b's is state[b]."""
+    L = lib()
+    s, hq, hk, hv = _sizes(q, k, v, 3, scale)
+    B, Hkv = s.batch, s.kv_heads
+    if state.dim() != 4 or state.shape[0] > 0x7fffffff:
+        raise ValueError("state must be [n, Hkv, Dk, Dv]")
+    n = state.shape[0]
+    o = torch.empty((B, s.q_heads, s.value_dim), dtype=q.dtype, device=q.device) if out is None else out
+    _check(L.zo_linear_attention_step(
+        C.byref(s), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(_heads(o, "out", (B, s.q_heads, s.value_dim), q)),
+        _flat(log_decay, "log_decay", torch.float32, (Hkv,), q),
+        _flat(state, "state", torch.float32, (n, Hkv, s.key_dim, s.value_dim), q), n,
+        _flat(slots, "slots", torch.int32, (B,), q), _stream(stream)))
+    _on_stream(stream, o)
+    return o
+
+
+# ---- layer norm ----
+
+def _rows(t: torch.Tensor, name: str, shape=None, like: torch.Tensor | None = None):
+    """(rows, D, stride between rows) of [..., D], whose rows must lie at equal distances."""
+    _device(t, name, None if like is None else like.dtype, like)
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.dim() < 1 or t.shape[-1] < 1:
+        raise ValueError(f"{name} must be [..., D] with D >= 1")
+    D = t.shape[-1]
+    if t.is_contiguous():
+        return t.numel() // D, D, D
+    if t.stride(-1) != 1 and D != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    try:
+        flat = t.view(-1, D)
+    except RuntimeError:
+        raise ValueError(f"the rows of {name} must lie at equal distances") from None
+    return flat.shape[0], D, flat.stride(0)
+
+
+def _norm_params(weight, bias, D, like):
+    w = weight if weight is not None else bias
+    wtype = like.dtype if w is None else w.dtype
+    if wtype not in _DTYPES:
+        raise ValueError(f"weight and bias must be float32 or bfloat16, got {wtype}")
+    return (_DTYPES[wtype], _flat(weight, "weight", wtype, (D,), like), _flat(bias, "bias", wtype, (D,), like))
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+               eps: float = 1e-5, out: torch.Tensor | None = None, stream=None):
+    """Layer norm over the last dimension: returns (y, mean, rstd), asynchronously; y of x's
+    type and shape (out, which may be x, or a new tensor), mean and rstd fp32 [rows] for the
+    backward pass. weight and bias [D], fp32 or bf16, or None."""
+    L = lib()
+    rows, D, xs = _rows(x, "x")
+    wtype, w, b = _norm_params(weight, bias, D, x)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    ys = D if out is None else _rows(y, "out", x.shape, x)[2]
+    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    sp = stats.data_ptr()
+    _check(L.zo_layer_norm(_DTYPES[x.dtype], wtype, rows, D, x.data_ptr(), xs, w, b, eps, y.data_ptr(), ys, sp,
+                           sp + 4 * rows, _stream(stream)))
+    _on_stream(stream, y, stats)
+    return y, stats[0], stats[1]
+
+
+def layer_norm_workspace_bytes(rows: int, D: int) -> int:
+    return int(lib().zo_layer_norm_workspace_bytes(rows, D))
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor | None, mean: torch.Tensor,
+                        rstd: torch.Tensor, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                        stream=None):
+    """Returns (dx, dweight, dbias), asynchronously: dx of x's type and shape (out, which may
+    be dy or x, or a new tensor), dweight and dbias fp32 [D], summed in a fixed order."""
+    L = lib()
+    rows, D, xs = _rows(x, "x")
+    dys = _rows(dy, "dy", x.shape, x)[2]
+    wtype, w, _ = _norm_params(weight, None, D, x)
+    mp = _flat(mean, "mean", torch.float32, (rows,), x)
+    rp = _flat(rstd, "rstd", torch.float32, (rows,), x)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    dxs = D if out is None else _rows(dx, "out", x.shape, x)[2]
+    dw = torch.empty((2, D), dtype=torch.float32, device=x.device)
+    dp = dw.data_ptr()
+    ws, wp, wn = _workspace(workspace, L.zo_layer_norm_workspace_bytes(rows, D), x)
+    _check(L.zo_layer_norm_backward(_DTYPES[x.dtype], wtype, rows, D, dy.data_ptr(), dys, x.data_ptr(), xs, w, mp, rp,
+                                    dx.data_ptr(), dxs, dp, dp + 4 * D, wp, wn, _stream(stream)))
+    _on_stream(stream, dx, dw, ws)
+    return dx, dw[0], dw[1]
+
+
+# ---- AdamW ----
+
+class AdamW:
+    """AdamW over a list of parameter tensors, all in one launch for up to 64 of them.
+
+    params: contiguous device tensors, fp32 or bf16, updated in place. weight_decay: one
+    number, or one for each tensor. state_bits: 32 (m and v fp32) or 8 (m int8 and v uint8
+    codes with m_scale and v_scale, the largest values of blocks of 256: see
+    zo_layers.h). The moments of tensor i begin at offsets[i] of the flat m and v and take
+    whole blocks. step_count is the number of steps done; a checkpoint is step_count, m, v
+    and the scales."""
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0,
+                 state_bits: int = 32):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("no parameters")
+        if state_bits not in (32, 8):
+            raise ValueError("state_bits must be 32 or 8")
+        first = self.params[0]
+        for i, p in enumerate(self.params):
+            _device(p, f"params[{i}]", None, first)
+            if not p.is_contiguous():
+                raise ValueError(f"params[{i}] must be contiguous")
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(self.params)
+        if len(decay) != len(self.params):
+            raise ValueError(f"{len(decay)} weight decays for {len(self.params)} tensors")
+        self.lr, self.betas, self.eps, self.state_bits, self.step_count = lr, tuple(betas), eps, state_bits, 0
+        self.offsets, at = [], 0
+        for p in self.params:
+            self.offsets.append(at)
+            at += (p.numel() + BLOCK - 1) // BLOCK * BLOCK
+        dev = first.device
+        self.m_scale = self.v_scale = None
+        if state_bits == 8:
+            self.m = torch.zeros(at, dtype=torch.int8, device=dev)
+            self.v = torch.zeros(at, dtype=torch.uint8, device=dev)
+            self.m_scale = torch.zeros(at // BLOCK, dtype=torch.float32, device=dev)
+            self.v_scale = torch.zeros(at // BLOCK, dtype=torch.float32, device=dev)
+        else:
+            self.m = torch.zeros(at, dtype=torch.float32, device=dev)
+            self.v = torch.zeros(at, dtype=torch.float32, device=dev)
+        self._shapes = [p.shape for p in self.params]
+        self._table = (_Tensor * len(self.params))(
+            *(_Tensor(p.data_ptr(), None, p.numel(), o, float(d), _DTYPES[p.dtype], zo.FP32)
+              for p, o, d in zip(self.params, self.offsets, decay)))
+
+    def step(self, grads, grad_scale: torch.Tensor | None = None, skipped: torch.Tensor | None = None, stream=None):
+        """One step (asynchronous) with one contiguous fp32 or bf16 gradient for each tensor.
+        grad_scale (device fp32 [1]) multiplies them; if it is not finite the step changes
+        nothing, and skipped (device int32 [1]) is set to 1, else to 0. step_count goes up
+        either way."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError(f"{len(grads)} gradients for {len(self.params)} tensors")
+        dev = self.m.device
+        for t, p, shape, g in zip(self._table, self.params, self._shapes, grads):
+            if g.device != dev or g.shape != shape or not g.is_contiguous() or g.dtype not in _DTYPES:
+                raise ValueError(f"gradients must be contiguous fp32 or bf16 tensors of their parameters' shapes on "
+                                 f"{dev}: got {g.dtype} {list(g.shape)} on {g.device} for {list(shape)}")
+            t.param, t.grad, t.gdtype = p.data_ptr(), g.data_ptr(), _DTYPES[g.dtype]
+        like = self.m
+        gs = _flat(grad_scale, "grad_scale", torch.float32, (1,), like)
+        sk = _flat(skipped, "skipped", torch.int32, (1,), like)
+        cfg = _AdamWConfig(self.lr, self.betas[0], self.betas[1], self.eps, self.step_count + 1, self.state_bits)
+        eight = self.state_bits == 8
+        _check(lib().zo_adamw(C.byref(cfg), self._table, len(grads), self.m.data_ptr(), self.v.data_ptr(),
+                              self.m_scale.data_ptr() if eight else None, self.v_scale.data_ptr() if eight else None,
+                              gs, sk, _stream(stream)))
+        self.step_count += 1
+
+    def moments(self, stream=None):
+        """The flat fp32 (m, v): the buffers themselves (32 bits), or the values that the codes stand for."""
+        if self.state_bits == 32:
+            return self.m, self.v
+        m = torch.empty(self.m.numel(), dtype=torch.float32, device=self.m.device)
+        v = torch.empty_like(m)
+        _check(lib().zo_adamw_moments(m.numel(), self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr(),
+                                      self.v_scale.data_ptr(), m.data_ptr(), v.data_ptr(), _stream(stream)))
+        _on_stream(stream, m, v)
+        return m, v

@@ -1,0 +1,340 @@
+"""Linear attention with a decay for each head on the GPU (forward, backward and
+the step for single tokens) against the recurrence in 64 bits, at the lengths,
+head sizes, layouts and masks where it can go wrong."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import layers_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def layers():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2505_17852_amd import layers as m
+    m.lib()
+    return m
+
+
+def rand(rng, shape, dtype="f32", scale=1.0):
+    """(device tensor, its values on the host)."""
+    t = torch.from_numpy((scale * rng.standard_normal(shape)).astype(np.float32)).to(DT[dtype])
+    return t.cuda(), t.float().numpy()
+
+
+def host(t):
+    return None if t is None else t.detach().float().cpu().numpy()
+
+
+def close(name, got, want, bound):
+    off = np.abs(host(got).astype(np.float64) - want)
+    worst = float((off / bound).max()) if off.size else 0.0
+    print(f"{name}: worst error {worst:.3f} of its bound", flush=True)
+    assert np.isfinite(host(got)).all() and worst <= 1.0, name
+
+
+def make(rng, dtype, B, T, Hq, Hkv, Dk, Dv, state=False, lengths=None, decay=None):
+    s = dict(dtype=dtype, scale=ref.default_scale(Dk), log_decay=ref.log_decays(Hkv) if decay is None else decay)
+    for name, shape in (("q", (B, T, Hq, Dk)), ("k", (B, T, Hkv, Dk)), ("v", (B, T, Hkv, Dv)),
+                        ("do", (B, T, Hq, Dv))):
+        s[name + "_d"], s[name] = rand(rng, shape, dtype)
+    for name in ("initial", "dfinal"):
+        s[name + "_d"], s[name] = rand(rng, (B, Hkv, Dk, Dv)) if state else (None, None)
+    s["lengths"] = lengths
+    s["lengths_d"] = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    s["decay_d"] = torch.from_numpy(np.asarray(s["log_decay"], dtype=np.float32)).cuda()
+    return s
+
+
+def check_forward(layers, s, **kw):
+    B, T, Hq, Dk = s["q"].shape
+    Dv = s["v"].shape[3]
+    o, final = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], scale=s["scale"],
+                                       initial_state=s["initial_d"], lengths=s["lengths_d"], return_state=True, **kw)
+    want, wfinal, mag, fmag = ref.attention(s["q"], s["k"], s["v"], s["log_decay"], s["scale"], s["initial"], s["lengths"])
+    n = ref.attention_terms(T, Dk, Dv)
+    close("o", o, want, ref.attention_bound(want, mag, s["dtype"], n))
+    close("final", final, wfinal, ref.state_bound(fmag, s["dtype"], n))
+    return o, final
+
+
+def check_backward(layers, s):
+    B, T, Hq, Dk = s["q"].shape
+    Hkv, Dv = s["v"].shape[2:]
+    got = layers.linear_attention_backward(s["do_d"], s["q_d"], s["k_d"], s["v_d"], s["decay_d"], scale=s["scale"],
+                                           initial_state=s["initial_d"], lengths=s["lengths_d"],
+                                           dfinal_state=s["dfinal_d"], return_dinitial=True)
+    want, mag = ref.attention_backward(s["do"], s["q"], s["k"], s["v"], s["log_decay"], s["scale"], s["initial"],
+                                       s["lengths"], s["dfinal"])
+    n = ref.attention_terms(T * Hq // Hkv, Dk, Dv)
+    for name, g in zip(("dq", "dk", "dv"), got):
+        close(name, g, want[name], ref.attention_bound(want[name], mag[name], s["dtype"], n))
+    close("dinitial", got[3], want["dinitial"], ref.state_bound(mag["dinitial"], s["dtype"], n))
+    return got
+
+
+# B, T, Hq, Hkv, Dk, Dv, state, lengths
+SHAPES = {
+    "one_token": (2, 1, 2, 2, 64, 64, True, None),
+    "one_value": (1, 5, 1, 1, 1, 1, True, None),
+    "two_tokens": (1, 2, 4, 1, 32, 32, False, None),
+    "odd_heads": (2, 37, 3, 3, 40, 24, True, None),
+    "prime": (1, 67, 2, 1, 53, 61, True, None),
+    "unequal": (2, 64, 2, 2, 128, 32, True, None),
+    "unequal_other": (1, 65, 2, 2, 32, 128, False, None),
+    "chunks": (1, 192, 2, 2, 64, 64, False, None),
+    "shared": (2, 130, 6, 2, 64, 64, True, None),
+    "wide": (1, 129, 2, 2, 128, 128, True, None),
+    "widest": (1, 70, 2, 1, 256, 256, True, None),
+    "wide_odd": (1, 70, 1, 1, 200, 129, True, None),
+    "ragged": (6, 150, 4, 2, 64, 64, True, [0, 1, 150, 64, 65, 127]),
+    "ragged_no_state": (3, 100, 2, 2, 32, 48, False, [99, 0, 33]),
+    "empty_all": (2, 20, 2, 1, 32, 32, True, [0, 0]),
+    "lengths_outside": (3, 40, 1, 1, 64, 64, True, [-5, 1000, 40]),
+    "long": (1, 1500, 2, 1, 64, 64, True, None),
+    "long_ragged": (2, 1111, 1, 1, 128, 128, True, [1111, 600]),
+}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", list(SHAPES))
+def test_forward_and_backward(layers, name, dtype):
+    B, T, Hq, Hkv, Dk, Dv, state, lengths = SHAPES[name]
+    s = make(np.random.default_rng(len(name) + 17), dtype, B, T, Hq, Hkv, Dk, Dv, state, lengths)
+    check_forward(layers, s)
+    check_backward(layers, s)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_decays_at_their_ends(layers, dtype):
+    """No decay, total decay (log 0), and one that underflows within a chunk."""
+    decay = np.array([0.0, -np.inf, -3.0, -40.0], dtype=np.float32)
+    s = make(np.random.default_rng(3), dtype, 2, 150, 4, 4, 32, 32, True, [150, 77], decay)
+    check_forward(layers, s)
+    check_backward(layers, s)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_slices_strides_and_orders(layers, dtype):
+    """q, k and v as slices of one projection, batch and position swapped in memory, odd addresses."""
+    B, T, Hq, Hkv, D = 3, 70, 4, 2, 40
+    rng = np.random.default_rng(5)
+    flat, _ = rand(rng, T * B * (Hq + 2 * Hkv) * D + 1, dtype)
+    qkv = flat[1:].view(T, B, (Hq + 2 * Hkv), D).transpose(0, 1)
+    s = make(rng, dtype, B, T, Hq, Hkv, D, D, True)
+    for name, at, n in (("q", 0, Hq), ("k", Hq, Hkv), ("v", Hq + Hkv, Hkv)):
+        s[name + "_d"] = qkv[:, :, at:at + n]
+        s[name] = host(s[name + "_d"])
+    o, _ = check_forward(layers, s)
+    check_backward(layers, s)
+    # the output into a view: heads reversed in memory by their order, gaps between positions
+    room = torch.full((B, T, 2, Hq, D), 7.0, dtype=DT[dtype], device="cuda")
+    o2, _ = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], scale=s["scale"],
+                                    initial_state=s["initial_d"], out=room[:, :, 0])
+    assert torch.equal(o2, o) and bool((room[:, :, 1] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_values_past_the_lengths_are_never_used(layers, dtype):
+    """NaN and infinities past the lengths change nothing; outputs and gradients there are zero."""
+    lengths = [0, 1, 63, 64, 100]
+    s = make(np.random.default_rng(8), dtype, 5, 130, 2, 1, 64, 64, True, lengths)
+    a = [*check_forward(layers, s), *check_backward(layers, s)]
+    for name in ("q", "k", "v", "do"):
+        for b, n in enumerate(lengths):
+            s[name + "_d"][b, n:] = float("nan") if b % 2 else float("inf")
+    o, final = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], scale=s["scale"],
+                                       initial_state=s["initial_d"], lengths=s["lengths_d"], return_state=True)
+    grads = layers.linear_attention_backward(s["do_d"], s["q_d"], s["k_d"], s["v_d"], s["decay_d"], scale=s["scale"],
+                                             initial_state=s["initial_d"], lengths=s["lengths_d"],
+                                             dfinal_state=s["dfinal_d"], return_dinitial=True)
+    for x, y in zip(a, (o, final, *grads)):
+        assert torch.equal(x, y)
+    for b, n in enumerate(lengths):
+        assert not o[b, n:].any() and not any(g[b, n:].any() for g in grads[:3])
+    assert torch.equal(final[0], s["initial_d"][0]) and torch.equal(grads[3][0], s["dfinal_d"][0])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("at", [0, 9, 63, 64, 100])
+def test_a_bad_value_leaves_earlier_positions_alone(layers, dtype, bad, at):
+    """A value that is not finite, in v, k or q, reaches outputs from its position on only,
+    and in the backward pass (in do) gradients of k and v up to its position only."""
+    s = make(np.random.default_rng(13), dtype, 1, 130, 1, 1, 64, 64, False)
+    args = dict(scale=s["scale"])
+    base, _ = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], **args)
+    for name in ("v", "k", "q"):
+        x = {n: s[n + "_d"].clone() for n in "qkv"}
+        x[name][0, at, 0, 5] = bad
+        o, _ = layers.linear_attention(x["q"], x["k"], x["v"], s["decay_d"], **args)
+        assert torch.equal(o[:, :at], base[:, :at]), name
+        assert not torch.isfinite(o[0, at]).all(), name
+        if name == "q":
+            assert torch.equal(o[:, at + 1:], base[:, at + 1:])
+        if name == "v":
+            other = torch.ones(64, dtype=torch.bool, device="cuda")
+            other[5] = False
+            assert torch.equal(o[..., other], base[..., other]) and not torch.isfinite(o[0, at:, 0, 5]).any()
+    grads = layers.linear_attention_backward(s["do_d"], s["q_d"], s["k_d"], s["v_d"], s["decay_d"], **args)
+    x = s["do_d"].clone()
+    x[0, at, 0, 5] = bad
+    got = layers.linear_attention_backward(x, s["q_d"], s["k_d"], s["v_d"], s["decay_d"], **args)
+    for g, w in zip(got[1:3], grads[1:3]):
+        assert torch.equal(g[:, at + 1:], w[:, at + 1:])
+    for t in (slice(0, at), slice(at + 1, None)):
+        assert torch.equal(got[0][:, t], grads[0][:, t])
+
+
+def test_gradients_against_differences(layers):
+    """Directional differences of a loss of the output and the final state (fp32): f is
+    quadratic in q, k and v together, so central differences are exact but for rounding,
+    which the step size keeps at 1e-3 of the change."""
+    s = make(np.random.default_rng(21), "f32", 2, 90, 4, 2, 32, 32, True, [90, 51])
+    rng = np.random.default_rng(22)
+    grads = dict(zip(("q", "k", "v", "initial"), layers.linear_attention_backward(
+        s["do_d"], s["q_d"], s["k_d"], s["v_d"], s["decay_d"], scale=s["scale"], initial_state=s["initial_d"],
+        lengths=s["lengths_d"], dfinal_state=s["dfinal_d"])))
+
+    def loss(name, x):
+        a = {n: s[n + "_d"] for n in ("q", "k", "v", "initial")}
+        a[name] = x
+        o, final = layers.linear_attention(a["q"], a["k"], a["v"], s["decay_d"], scale=s["scale"],
+                                           initial_state=a["initial"], lengths=s["lengths_d"], return_state=True)
+        return float((o.double() * s["do_d"].double()).sum() + (final.double() * s["dfinal_d"].double()).sum())
+
+    for name in grads:
+        d = grads[name] + 0.3 * grads[name].norm() / np.sqrt(grads[name].numel()) * rand(rng, s[name].shape)[0]
+        want = ref.finite_difference(lambda x: loss(name, x), s[name + "_d"], d, 0.5 / float(d.abs().max()))
+        got = float((grads[name].double() * d.double()).sum())
+        print(f"d{name}: {got} difference {want}", flush=True)
+        assert abs(got - want) <= 2e-3 * abs(want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_prompt_in_parts_is_the_prompt(layers, dtype):
+    """The state handed from part to part, then to single tokens, in place."""
+    B, T, Hq, Hkv, D = 2, 140, 4, 2, 64
+    s = make(np.random.default_rng(31), dtype, B, T, Hq, Hkv, D, D, True)
+    want, wfinal, mag, fmag = ref.attention(s["q"], s["k"], s["v"], s["log_decay"], s["scale"], s["initial"])
+    state, parts = s["initial_d"].clone(), []
+    for a, b in ((0, 1), (1, 70), (70, 70), (70, 134)):
+        o, final = layers.linear_attention(s["q_d"][:, a:b], s["k_d"][:, a:b], s["v_d"][:, a:b], s["decay_d"],
+                                           scale=s["scale"], initial_state=state, final_state=state)
+        assert final is state
+        parts.append(o)
+    for t in range(134, T):
+        parts.append(layers.linear_attention_step(s["q_d"][:, t], s["k_d"][:, t], s["v_d"][:, t], s["decay_d"], state,
+                                                  scale=s["scale"]).unsqueeze(1))
+    n = ref.attention_terms(T, D, D)
+    close("o", torch.cat(parts, 1), want, ref.attention_bound(want, mag, dtype, n))
+    close("state", state, wfinal, ref.state_bound(fmag, dtype, n))
+
+
+STEPS = {
+    "one": (1, 1, 1, 1, 1),
+    "small": (3, 2, 2, 32, 32),
+    "odd": (5, 6, 3, 53, 61),
+    "unaligned": (2, 3, 1, 129, 66),
+    "shared": (4, 18, 2, 64, 64),
+    "wide": (2, 2, 2, 256, 256),
+    "plain": (7, 4, 4, 128, 128),
+}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", list(STEPS))
+def test_step(layers, name, dtype):
+    B, Hq, Hkv, Dk, Dv = STEPS[name]
+    s = make(np.random.default_rng(len(name)), dtype, B, 1, Hq, Hkv, Dk, Dv, True)
+    want, wfinal, mag, fmag = ref.attention(s["q"], s["k"], s["v"], s["log_decay"], s["scale"], s["initial"])
+    state = s["initial_d"].clone()
+    o = layers.linear_attention_step(s["q_d"][:, 0], s["k_d"][:, 0], s["v_d"][:, 0], s["decay_d"], state,
+                                     scale=s["scale"])
+    n = ref.attention_terms(1, Dk, Dv)
+    # everything in fp32, the output rounded once
+    close("o", o, want[:, 0], ref.unit(dtype) * np.abs(want[:, 0]) + n * 2.0 ** -24 * mag[:, 0] + 1e-37)
+    close("state", state, wfinal, ref.state_bound(fmag, "f32", n))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_step_with_slots(layers, dtype):
+    """States anywhere in a pool, sequences without one, and slots that do not exist."""
+    B, Hq, Hkv, Dk, Dv, n = 6, 4, 2, 64, 40, 9
+    rng = np.random.default_rng(77)
+    s = make(rng, dtype, B, 1, Hq, Hkv, Dk, Dv)
+    pool, pool_h = rand(rng, (n, Hkv, Dk, Dv))
+    slots = [8, -1, 0, 9, 3, -2]
+    o = layers.linear_attention_step(s["q_d"][:, 0], s["k_d"][:, 0], s["v_d"][:, 0], s["decay_d"], pool,
+                                     scale=s["scale"], slots=torch.tensor(slots, dtype=torch.int32, device="cuda"))
+    live = [b for b, x in enumerate(slots) if 0 <= x < n]
+    at = [slots[b] for b in live]
+    want, wfinal, mag, fmag = ref.attention(s["q"][live], s["k"][live], s["v"][live], s["log_decay"], s["scale"],
+                                            pool_h[at])
+    t = ref.attention_terms(1, Dk, Dv)
+    close("o", o[live], want[:, 0], ref.unit(dtype) * np.abs(want[:, 0]) + t * 2.0 ** -24 * mag[:, 0] + 1e-37)
+    close("state", pool[at], wfinal, ref.state_bound(fmag, "f32", t))
+    rest = [i for i in range(n) if i not in at]
+    assert np.array_equal(host(pool)[rest], pool_h[rest])
+    assert not o[1].any() and torch.isnan(o[3]).all() and torch.isnan(o[5]).all()
+
+
+def test_the_same_bits_every_time(layers):
+    s = make(np.random.default_rng(41), "bf16", 2, 500, 4, 2, 64, 64, True, [500, 321])
+    runs = []
+    for _ in range(2):
+        runs.append([*layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], initial_state=s["initial_d"],
+                                              lengths=s["lengths_d"], return_state=True),
+                     *layers.linear_attention_backward(s["do_d"], s["q_d"], s["k_d"], s["v_d"], s["decay_d"],
+                                                       initial_state=s["initial_d"], lengths=s["lengths_d"],
+                                                       dfinal_state=s["dfinal_d"])])
+    assert all(torch.equal(x, y) for x, y in zip(*runs))
+
+
+def test_another_stream_and_a_graph(layers):
+    """On a stream of the caller's, and captured: every replay gives the eager result."""
+    s = make(np.random.default_rng(51), "bf16", 2, 700, 4, 2, 64, 64, True)
+    args = (s["q_d"], s["k_d"], s["v_d"], s["decay_d"])
+
+    def call(**kw):
+        return [*layers.linear_attention(*args, initial_state=s["initial_d"], return_state=True, **kw),
+                *layers.linear_attention_backward(s["do_d"], *args, initial_state=s["initial_d"],
+                                                  dfinal_state=s["dfinal_d"], **kw)]
+
+    want = call()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = call(stream=side)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call()
+    for _ in range(3):
+        for t in held:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(held, want))
+
+
+def test_nothing_to_do(layers):
+    """No sequences, or no positions: the states pass through."""
+    z = torch.zeros(0, 4, 2, 32, device="cuda")
+    decay = torch.zeros(2, device="cuda")
+    o, final = layers.linear_attention(z, z, z, decay, return_state=True)
+    assert o.shape == (0, 4, 2, 32) and final.shape == (0, 2, 32, 32)
+    z = torch.zeros(3, 0, 2, 32, device="cuda")
+    initial = torch.randn(3, 2, 32, 32, device="cuda")
+    o, final = layers.linear_attention(z, z, z, decay, initial_state=initial, return_state=True)
+    assert torch.equal(final, initial)
+    got = layers.linear_attention_backward(z, z, z, z, decay, dfinal_state=initial, return_dinitial=True)
+    assert torch.equal(got[3], initial)
+    e = torch.zeros(0, 2, 32, device="cuda")
+    assert layers.linear_attention_step(e, e, e, decay, initial).shape == (0, 2, 32)
