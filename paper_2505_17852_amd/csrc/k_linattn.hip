@@ -7,8 +7,42 @@
 //   dv  R  = gamma (R + scale q do^T),    dv = (R + scale q do^T)^T k     backward, sum over query heads
 //   dk  R' = gamma (R' + scale do q^T),   dk = (R' + scale do q^T)^T v    backward, sum over query heads
 // so a pass reads x (the reader), y and z (the products' sides) and writes out
-// [positions][dz], with the state R [dx][dz]; a workgroup takes one sequence,
-// one output head and a slice of the columns dz.
+// [positions][dz], with the state R [dx][dz].
+//
+// In chunks of 64 positions (counted in the pass's direction; off = 1 forward,
+// 0 backward, where the state that is carried has decayed already):
+//   P_ij  = score gamma^(i-j) (x_i . y_j)   for j <= i
+//   out_i = sum_j P_ij z_j + carry gamma^(i+off) R^T x_i
+//   R     = gamma^64 R + sum_j upd gamma^(64-off-j) y_j z_j^T
+// every sum a matrix product. A workgroup of four waves walks over the chunks of
+// one sequence, head and slice of 64 columns of z with R in its accumulators:
+// x, y, z are read and out is written once per slice (the slices and passes of a
+// state run next to each other on one XCD, whose L2 serves the second reading).
+// Wave w has the chunk's rows 16 w .. 16 w + 15 and a quarter of R's rows.
+//
+// Operands. MFMA 16x16: A and B have the same lane layout, lane l = row (or column)
+// l % 16, contraction index group l / 16; the result has column l % 16 and
+// rows 4 (l / 16) + r. Scores are formed as P^T (y x^T), so that a lane holds
+// P_ij of its row i = l % 16 for j = 16 n + 4 (l / 16) + r: taken in that order of j,
+// the accumulators are the next product's operand as they are. The other operand of
+// the sums over j (columns of y and z by rows j) is read from row-major LDS tiles in the
+// same order: with the transposing LDS load (bf16), or by words (fp32). out is
+// formed transposed too, so that a lane holds 4 neighbouring columns of one row.
+//
+// Precision: fp32 accumulators and state. bf16 rounds P, and R where x reads it, to
+// bf16 (the rounding of an input each); the state's own sum takes gamma^(..) y in two
+// bf16 parts, 2^-17 of it left out, since what is lost there would stay for all later
+// positions. fp32 runs on fp32 MFMAs throughout.
+//
+// Rows past a sequence's length are read as zeros. P of later positions is set
+// to zero, not multiplied by it; a z that is not finite would still turn those zeros
+// into NaN, so chunks that hold one (seen when it is staged) take z without it
+// and add its products to the rows that it reaches.
+//
+// Few sequences: where the workgroups would not fill the chip the positions are split
+// into segments; a first launch runs only the state's sum of every segment
+// but the last, a second adds the segments up, and the main launch starts each
+// segment from its own state.
 #include <hip/hip_runtime.h>
 
 #include "zo_layers.hpp"
@@ -16,113 +50,533 @@
 namespace zo {
 namespace {
 
-constexpr int kCols = 64;
-constexpr int kRowGroups = 16;
+constexpr int kChunk = 64;    // positions
+constexpr int kSlice = 64;    // columns of z per workgroup
+constexpr int kThreads = 256;
+constexpr int kXcds = 8;
 
-// Position by position: the state in registers (thread t: columns 4 (t % 16) ..,
-// rows t / 16 + 16 i).
-template <typename T, int ROWS>
-__global__ __launch_bounds__(256) void linattn_token_kernel(LinCall c) {
-  __shared__ float xs[ROWS * kRowGroups];
-  __shared__ float ys[ROWS * kRowGroups];
-  __shared__ float part[4][kCols];
-  const LinPass& a = c.pass[blockIdx.z];
-  const int tid = threadIdx.x, c4 = (tid & 15) * 4, rg = tid >> 4;
-  const int slices = (a.dz + kCols - 1) / kCols;
-  const int64_t blk = block_id(), bh = blk / slices;
-  const int b = (int)(bh / a.out_heads), h = (int)(bh % a.out_heads);
-  if (b >= c.B) return;
-  const int col = (int)(blk % slices) * kCols;
-  const int state = h / a.share;  // the key/value head
-  const int n = c.lengths ? min(max(c.lengths[b], 0), c.T) : c.T;
-  T* out = (T*)a.out + b * a.ob + h * a.oh + col;
-  const float gamma = expf(c.log_decay[state]);
-  const int64_t state_at = ((int64_t)b * c.kv_heads + state) * a.dx * a.dz;
-  float s[ROWS][4];
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int r = rg + kRowGroups * i, z = col + c4 + e;
-      s[i][e] = a.init && r < a.dx && z < a.dz ? a.init[state_at + (a.state_t ? (int64_t)z * a.dx + r : (int64_t)r * a.dz + z)] : 0.0f;
-    }
-  for (int t = n; t < c.T; ++t)
-    if (tid < kCols && col + tid < a.dz) out[t * a.ot + tid] = from_f32<T>(0.0f);
-  for (int u = 0; u < n; ++u) {
-    const int64_t t = a.reverse ? n - 1 - u : u;
-    if (!a.reverse)
-#pragma unroll
-      for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] *= gamma;
-    for (int src = 0; src < a.sources; ++src) {
-      const int yh = state * a.sources + src;
-      __syncthreads();
-      for (int d = tid; d < ROWS * kRowGroups; d += 256) {
-        ys[d] = d < a.dx ? to_f32(((const T*)a.y.p)[b * a.y.b + t * a.y.t + yh * a.y.h + d]) : 0.0f;
-        if (src == 0) xs[d] = d < a.dx ? to_f32(((const T*)a.x.p)[b * a.x.b + t * a.x.t + h * a.x.h + d]) : 0.0f;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int z = col + c4 + e;
-        const float zv = z < a.dz ? a.upd * to_f32(((const T*)a.z.p)[b * a.z.b + t * a.z.t + yh * a.z.h + z]) : 0.0f;
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) s[i][e] = fmaf(ys[rg + kRowGroups * i], zv, s[i][e]);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float acc = 0;
-#pragma unroll
-      for (int i = 0; i < ROWS; ++i) acc = fmaf(xs[rg + kRowGroups * i], s[i][e], acc);
-      acc += __shfl_xor(acc, 16, 64);
-      acc += __shfl_xor(acc, 32, 64);
-      if ((tid & 63) < 16) part[tid >> 6][c4 + e] = acc;
-    }
-    __syncthreads();
-    if (tid < kCols && col + tid < a.dz)
-      out[t * a.ot + tid] = from_f32<T>(a.carry * ((part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid])));
-    if (a.reverse)
-#pragma unroll
-      for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] *= gamma;
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef short s8 __attribute__((ext_vector_type(8)));
+
+// Positions of a pass are split into `segments` of `length` (a multiple of kChunk).
+struct Plan {
+  int segments;
+  int length;
+  int64_t groups;            // (sequence, key/value head, segment)
+  int members;               // workgroups of a group: (pass, head, slice)
+  float* states[kLinPasses]; // [B][kv_heads][segments - 1][dx][dz]
+};
+
+// The contraction block of one operand register set (4 VGPRs a lane).
+template <typename T>
+struct Op;
+template <>
+struct Op<uint16_t> {
+  static constexpr int KB = 32;
+  typedef b8 Frag;
+  static __device__ __forceinline__ f4 mma(Frag a, Frag b, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
-  if (a.fin && h % a.share == 0)
+  // contraction along a row: 8 values from index 8 g
+  static __device__ __forceinline__ Frag along(const uint16_t* row, int g) { return *(const Frag*)(row + 8 * g); }
+  // contraction over rows: rows 4 g .. 4 g + 3 and 16 + 4 g .., column l % 16
+  static __device__ __forceinline__ Frag down(const uint16_t* tile, int stride, int g, int m) {
+    typedef __attribute__((address_space(3))) s4 Lds;
+    const uint16_t* p = tile + (4 * g + (m >> 2)) * stride + 4 * (m & 3);
+    const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)p);
+    const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(p + 16 * stride));
+    return __builtin_bit_cast(Frag, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+template <>
+struct Op<float> {
+  static constexpr int KB = 16;
+  typedef f4 Frag;
+  static __device__ __forceinline__ f4 mma(Frag a, Frag b, f4 c) {
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i)
+    for (int s = 0; s < 4; ++s) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], b[s], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ Frag along(const float* row, int g) { return *(const Frag*)(row + 4 * g); }
+  static __device__ __forceinline__ Frag down(const float* tile, int stride, int g, int m) {
+    Frag f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = rg + kRowGroups * i, z = col + c4 + e;
-        if (r < a.dx && z < a.dz) a.fin[state_at + (a.state_t ? (int64_t)z * a.dx + r : (int64_t)r * a.dz + z)] = s[i][e];
+    for (int s = 0; s < 4; ++s) f[s] = tile[(4 * g + s) * stride + m];
+    return f;
+  }
+};
+
+// 16 bytes of a row from column `col`, zeros from column d on.
+template <typename T, bool even>
+__device__ __forceinline__ u4 load16(const T* row, int col, int d) {
+  constexpr int EL = 16 / sizeof(T);
+  struct __attribute__((packed, aligned(sizeof(T)))) Any { u4 v; };
+  if (col + EL <= d) return ((const Any*)(row + col))->v;
+  if constexpr (even) {
+    return u4{0, 0, 0, 0};
+  } else {
+    u4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < EL; ++e)
+      if (col + e < d) {
+        if constexpr (sizeof(T) == 2) v[e / 2] |= (uint32_t)row[col + e] << (16 * (e & 1));
+        else v[e] = __float_as_uint(row[col + e]);
       }
+    return v;
+  }
 }
 
 template <typename T>
-hipError_t launch(const LinCall& c, hipStream_t st) {
-  int64_t blocks = 0;
-  int dx = 0;
+__device__ __forceinline__ bool any_not_finite(u4 v) {
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 2)
+      bad |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
+    else
+      bad |= (v[e] & 0x7f800000u) == 0x7f800000u;
+  }
+  return bad;
+}
+template <typename T>
+__device__ __forceinline__ typename Op<T>::Frag only_finite(typename Op<T>::Frag f) {
+  u4 v = __builtin_bit_cast(u4, f);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 2) {
+      if ((v[e] & 0x7f80u) == 0x7f80u) v[e] &= 0xffff0000u;
+      if ((v[e] & 0x7f800000u) == 0x7f800000u) v[e] &= 0x0000ffffu;
+    } else {
+      if ((v[e] & 0x7f800000u) == 0x7f800000u) v[e] = 0;
+    }
+  }
+  return __builtin_bit_cast(typename Op<T>::Frag, v);
+}
+
+// gamma^n; gamma^0 is 1 whatever gamma.
+__device__ __forceinline__ float decay(float lg, int n) { return n == 0 ? 1.0f : exp2f(lg * (float)n); }
+
+template <typename T, int DX, bool even, bool state_only>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void linattn_chunk_kernel(LinCall c, Plan pl) {
+  typedef Op<T> O;
+  typedef typename O::Frag Frag;
+  constexpr int EL = 16 / sizeof(T), KB = O::KB;
+  constexpr int YS = DX + EL, ZS = kSlice + EL;       // rows of the tiles, 16 bytes apart from a multiple of the banks
+  constexpr int NY = kChunk * DX / EL / kThreads, NZ = kChunk * kSlice / EL / kThreads;
+  constexpr int NX = DX / KB, NJ = kChunk / KB;        // operand sets along a row of x, over the chunk's positions
+  constexpr int MW = DX / 64;                          // tiles of 16 rows of R per wave
+  __shared__ __align__(16) T ys[kChunk * YS];
+  __shared__ __align__(16) T zs[kChunk * ZS];
+  __shared__ __align__(16) T rs[state_only ? 1 : kSlice * YS];  // R^T where x reads it
+  __shared__ int bad[2];
+
+  // groups go round the XCDs (workgroup i runs on XCD i % 8), the members of one stay together
+  const int64_t id = block_id(), turn = id / kXcds;
+  const int64_t group = turn / pl.members * kXcds + id % kXcds;
+  if (group >= pl.groups) return;
+  int member = (int)(turn % pl.members), pass = 0;
+  for (;; ++pass) {
+    const int n = (state_only ? 1 : c.pass[pass].heads) * ((c.pass[pass].dz + kSlice - 1) / kSlice);
+    if (member < n) break;
+    member -= n;
+  }
+  const LinPass& a = c.pass[pass];
+  const int slices = (a.dz + kSlice - 1) / kSlice;
+  const int col = member % slices * kSlice;
+  const int seg = (int)(group % (pl.segments - (state_only ? 1 : 0)));
+  const int64_t bh = group / (pl.segments - (state_only ? 1 : 0));
+  const int b = (int)(bh / c.kv_heads), kvh = (int)(bh % c.kv_heads);
+  const int h = kvh * a.heads + member / slices;
+
+  const int n = c.lengths ? min(max(c.lengths[b], 0), c.T) : c.T;
+  const int r0 = seg * pl.length, r1 = min(n, r0 + pl.length);  // the segment's positions
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, m = lane & 15;
+  const float lg = c.log_decay[kvh] * 1.44269504088896340736f;
+  const int off = a.reverse ? 0 : 1;
+
+  T* out = (T*)a.out + b * a.ob + (int64_t)h * a.oh;
+  if constexpr (state_only) {
+    if (r0 + pl.length > n) return;  // no position follows it
+  } else {
+    const int end = min(c.T, r0 + pl.length), width = min(kSlice, a.dz - col);
+    for (int t = max(r0, n) + w; t < end; t += kThreads / 64)
+      if (lane < width) out[t * a.ot + col + lane] = from_f32<T>(0.0f);
+    if (r0 >= n && seg > 0) return;
+  }
+
+  // R: rows 16 (w MW + i) + 4 g + r, columns col + 16 j + m
+  f4 R[MW][4];
+  {
+    const float* from = nullptr;
+    bool turned = false;
+    if (seg == 0) {
+      if (a.init) from = a.init + bh * a.dx * a.dz;
+      turned = a.state_t;
+    } else if (!state_only) {
+      from = pl.states[pass] + (bh * (pl.segments - 1) + seg - 1) * a.dx * a.dz;
+    }
+#pragma unroll
+    for (int i = 0; i < MW; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int x = 16 * (w * MW + i) + 4 * g + r, z = col + 16 * j + m;
+          R[i][j][r] = from && x < a.dx && z < a.dz ? from[turned ? z * a.dx + x : x * a.dz + z] : 0.0f;
+        }
+  }
+
+  // factors of a whole chunk: P's by (row, position), y's by position
+  const int row = 16 * w + m;
+  float pf[4][4], yf[NJ][KB / 4];
+  if constexpr (!state_only)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int apart = row - (16 * j + 4 * g + r);
+        pf[j][r] = apart >= 0 ? a.score * decay(lg, apart) : 0.0f;
+      }
+  const float xf = state_only ? 0.0f : a.carry * decay(lg, row + off);
+  const auto y_factors = [&](int rows) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < KB / 4; ++e) {
+        const int at = KB * j + 16 * (e >> 2) + 4 * g + (e & 3);
+        yf[j][e] = at < rows ? a.upd * decay(lg, rows - off - at) : 0.0f;
+      }
+  };
+  y_factors(kChunk);
+  float rf = decay(lg, kChunk);
+
+  // staging: the next step's y and z, the next chunk's x
+  u4 yn[NY], zn[NZ];
+  Frag xc[NX], xn[NX];
+  const auto position = [&](int r) -> int64_t { return a.reverse ? n - 1 - r : r; };
+  const auto fetch_yz = [&](int start, int src) {
+    const int64_t head = (int64_t)kvh * a.sources + src;
+    const T* y = (const T*)a.y.p + b * a.y.b + head * a.y.h;
+    const T* z = (const T*)a.z.p + b * a.z.b + head * a.z.h;
+#pragma unroll
+    for (int i = 0; i < NY; ++i) {
+      const int at = tid + kThreads * i, r = start + at / (DX / EL), q = at % (DX / EL) * EL;
+      yn[i] = r < r1 ? load16<T, even>(y + position(r) * a.y.t, q, a.dx) : u4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < NZ; ++i) {
+      const int at = tid + kThreads * i, r = start + at / (kSlice / EL), q = at % (kSlice / EL) * EL;
+      zn[i] = r < r1 ? load16<T, even>(z + position(r) * a.z.t, col + q, a.dz) : u4{0, 0, 0, 0};
+    }
+  };
+  const auto fetch_x = [&](int start) {
+    const int r = start + row;
+    const T* x = (const T*)a.x.p + b * a.x.b + (int64_t)h * a.x.h + (r < r1 ? position(r) * a.x.t : 0);
+#pragma unroll
+    for (int i = 0; i < NX; ++i)
+      xn[i] = __builtin_bit_cast(Frag, r < r1 ? load16<T, even>(x, i * KB + KB / 4 * g, a.dx) : u4{0, 0, 0, 0});
+  };
+
+  if (r0 < r1) {
+    fetch_yz(r0, 0);
+    if constexpr (!state_only) fetch_x(r0);
+  }
+  if (tid < 2) bad[tid] = 0;
+  __syncthreads();
+  f4 acc[4];
+  int step = 0, src = 0;
+  for (int start = r0; start < r1; ++step) {
+    const int rows = min(kChunk, r1 - start);
+#pragma unroll
+    for (int i = 0; i < NY; ++i) {
+      const int at = tid + kThreads * i;
+      *(u4*)(ys + at / (DX / EL) * YS + at % (DX / EL) * EL) = yn[i];
+    }
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < NZ; ++i) {
+      const int at = tid + kThreads * i;
+      *(u4*)(zs + at / (kSlice / EL) * ZS + at % (kSlice / EL) * EL) = zn[i];
+      if constexpr (!state_only) found |= any_not_finite<T>(zn[i]);
+    }
+    if constexpr (!state_only) {
+      if (found) bad[step & 1] = 1;
+      if (src == 0) {
+#pragma unroll
+        for (int i = 0; i < NX; ++i) xc[i] = xn[i];
+#pragma unroll
+        for (int i = 0; i < MW; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) store_run<T, 4>(rs + (16 * j + m) * YS + 16 * (w * MW + i) + 4 * g, (const float*)&R[i][j]);
+      }
+    }
+    __syncthreads();
+    const bool flagged = !state_only && bad[step & 1];
+    if (tid == 0) bad[(step + 1) & 1] = 0;
+    // the next step's loads
+    const bool last_src = src == a.sources - 1;
+    if (!last_src) {
+      fetch_yz(start, src + 1);
+    } else if (start + kChunk < r1) {
+      fetch_yz(start + kChunk, 0);
+      if constexpr (!state_only) fetch_x(start + kChunk);
+    }
+    if (src == 0 && rows < kChunk) {
+      y_factors(rows);
+      rf = decay(lg, rows);
+    }
+    f4 P[4];
+    Frag pb[NJ];
+    if constexpr (!state_only) {
+      if (src == 0) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          acc[j] = f4{0, 0, 0, 0};
+#pragma unroll
+          for (int i = 0; i < NX; ++i) acc[j] = O::mma(O::along(rs + (16 * j + m) * YS + i * KB, g), xc[i], acc[j]);
+          acc[j] *= xf;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        P[j] = f4{0, 0, 0, 0};
+        if (j > w) continue;
+#pragma unroll
+        for (int i = 0; i < NX; ++i) P[j] = O::mma(O::along(ys + (16 * j + m) * YS + i * KB, g), xc[i], P[j]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) P[j][r] = 16 * j + 4 * g + r <= row ? P[j][r] * pf[j][r] : 0.0f;
+      }
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+          pb[j] = __builtin_bit_cast(Frag, u4{bf16_pair(P[2 * j][0], P[2 * j][1]), bf16_pair(P[2 * j][2], P[2 * j][3]),
+                                              bf16_pair(P[2 * j + 1][0], P[2 * j + 1][1]),
+                                              bf16_pair(P[2 * j + 1][2], P[2 * j + 1][3])});
+      } else {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) pb[j] = P[j];
+      }
+    }
+    if (src == 0)
+#pragma unroll
+      for (int i = 0; i < MW; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) R[i][j] *= rf;
+#pragma unroll
+    for (int k = 0; k < NJ; ++k) {
+      Frag z[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) z[j] = O::down(zs + k * KB * ZS + 16 * j, ZS, g, m);
+      if constexpr (!state_only) {
+        if (k * KB <= 16 * w + 15) {
+          if (!flagged) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = O::mma(z[j], pb[k], acc[j]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = O::mma(only_finite<T>(z[j]), pb[k], acc[j]);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < MW; ++i) {
+        const Frag y = O::down(ys + k * KB * YS + 16 * (w * MW + i), YS, g, m);
+        if constexpr (sizeof(T) == 2) {
+          u4 hi, lo;
+          const u4 raw = __builtin_bit_cast(u4, y);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p = __uint_as_float(raw[e] << 16) * yf[k][2 * e];
+            const float q = __uint_as_float(raw[e] & 0xffff0000u) * yf[k][2 * e + 1];
+            hi[e] = bf16_pair(p, q);
+            lo[e] = bf16_pair(p - __uint_as_float(hi[e] << 16), q - __uint_as_float(hi[e] & 0xffff0000u));
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            R[i][j] = O::mma(__builtin_bit_cast(Frag, hi), z[j], R[i][j]);
+            R[i][j] = O::mma(__builtin_bit_cast(Frag, lo), z[j], R[i][j]);
+          }
+        } else {
+          Frag f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[e] = y[e] * yf[k][e];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) R[i][j] = O::mma(f, z[j], R[i][j]);
+        }
+      }
+    }
+    if constexpr (!state_only) {
+      if (flagged) {
+        // the products of z that are not finite, for the rows they reach
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+              const float p = __shfl(P[j][r], m + 16 * q, 64);
+              const int at = 16 * j + 4 * q + r;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float v = to_f32(zs[at * ZS + 16 * (e >> 2) + 4 * g + (e & 3)]);
+                if (at <= row && !(fabsf(v) < __builtin_inff())) acc[e >> 2][e & 3] += p * v;
+              }
+            }
+      }
+      if (last_src && row < rows) {
+        T* o = out + position(start + row) * a.ot;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int z = col + 16 * j + 4 * g;
+          if (z + 4 <= a.dz) {
+            store_run<T, 4>(o + z, (const float*)&acc[j]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (z + e < a.dz) o[z + e] = from_f32<T>(acc[j][e]);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    if (last_src) {
+      src = 0;
+      start += kChunk;
+    } else {
+      ++src;
+    }
+  }
+
+  float* to = nullptr;
+  bool turned = false;
+  if constexpr (state_only) {
+    to = pl.states[pass] + (bh * (pl.segments - 1) + seg) * a.dx * a.dz;
+  } else if (a.fin && r1 == n && h == kvh * a.heads) {  // the segment of the last position (the first one of none)
+    to = a.fin + bh * a.dx * a.dz;
+    turned = a.state_t;
+  }
+  if (to)
+#pragma unroll
+    for (int i = 0; i < MW; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int x = 16 * (w * MW + i) + 4 * g + r, z = col + 16 * j + m;
+          if (x < a.dx && z < a.dz) to[turned ? z * a.dx + x : x * a.dz + z] = R[i][j][r];
+        }
+}
+
+// Adds up the segments' states: state_s = gamma^length state_(s-1) + its own sum.
+__global__ __launch_bounds__(kThreads) void linattn_scan_kernel(LinCall c, Plan pl) {
+  const int pass = blockIdx.z;
+  const int per = c.pass[pass].dx * c.pass[pass].dz;
+  const int64_t blk = block_id();
+  const int parts = (per + kThreads - 1) / kThreads;
+  const int64_t bh = blk / parts;
+  if (bh >= (int64_t)c.B * c.kv_heads) return;
+  const int e = (int)(blk % parts) * kThreads + threadIdx.x;
+  if (e >= per) return;
+  const int b = (int)(bh / c.kv_heads);
+  const int n = c.lengths ? min(max(c.lengths[b], 0), c.T) : c.T;
+  const int whole = min(n / pl.length, pl.segments - 1);  // segments whose sums exist
+  const float gamma = decay(c.log_decay[bh % c.kv_heads] * 1.44269504088896340736f, pl.length);
+  float* p = pl.states[pass] + bh * (pl.segments - 1) * per + e;
+  float s = 0;
+  for (int i = 0; i < whole; ++i) {
+    const float u = p[(int64_t)i * per];
+    s = i == 0 ? u : fmaf(gamma, s, u);
+    p[(int64_t)i * per] = s;
+  }
+}
+
+// Segments of a call: enough workgroups for two on every CU, none shorter than four chunks.
+void split(int64_t workgroups, int T, int* segments, int* length) {
+  int64_t s = workgroups >= 256 || workgroups == 0 ? 1 : (512 + workgroups - 1) / workgroups;
+  const int64_t most = T / (4 * kChunk);
+  if (s > most) s = most;
+  if (s < 1) s = 1;
+  *length = (int)(((T + s - 1) / s + kChunk - 1) / kChunk * kChunk);
+  if (*length == 0) *length = kChunk;
+  *segments = T > 0 ? (T + *length - 1) / *length : 1;
+}
+
+int slices_of(int dz) { return (dz + kSlice - 1) / kSlice; }
+
+template <typename T, int DX, bool even>
+hipError_t launch_chunks(const LinCall& c, Plan pl, hipStream_t st) {
+  const int64_t states = (int64_t)c.B * c.kv_heads;
+  const auto grid = [&](int64_t groups, int members) {
+    return wide_grid((groups + kXcds - 1) / kXcds * kXcds * members);
+  };
+  int slices = 0, members = 0, most = 0;
   for (int i = 0; i < c.npasses; ++i) {
     const LinPass& p = c.pass[i];
-    blocks = std::max(blocks, (int64_t)c.B * p.out_heads * ((p.dz + kCols - 1) / kCols));
-    dx = std::max(dx, p.dx);
+    slices += slices_of(p.dz);
+    members += p.heads * slices_of(p.dz);
+    most = std::max(most, p.dx * p.dz);
   }
-  dim3 grid = wide_grid(blocks);
-  grid.z = c.npasses;
-  if (dx <= 64) linattn_token_kernel<T, 4><<<grid, 256, 0, st>>>(c);
-  else if (dx <= 128) linattn_token_kernel<T, 8><<<grid, 256, 0, st>>>(c);
-  else linattn_token_kernel<T, 16><<<grid, 256, 0, st>>>(c);
+  if (pl.segments > 1) {
+    pl.groups = states * (pl.segments - 1);
+    pl.members = slices;
+    linattn_chunk_kernel<T, DX, even, true><<<grid(pl.groups, slices), kThreads, 0, st>>>(c, pl);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (pl.segments > 2) {
+      dim3 g = wide_grid(states * ((most + kThreads - 1) / kThreads));
+      g.z = c.npasses;
+      linattn_scan_kernel<<<g, kThreads, 0, st>>>(c, pl);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
+  pl.groups = states * pl.segments;
+  pl.members = members;
+  linattn_chunk_kernel<T, DX, even, false><<<grid(pl.groups, members), kThreads, 0, st>>>(c, pl);
   return hipGetLastError();
+}
+
+template <typename T, bool even>
+hipError_t launch(const LinCall& c, const Plan& pl, int dx, hipStream_t st) {
+  if (dx <= 64) return launch_chunks<T, 64, even>(c, pl, st);
+  if (dx <= 128) return launch_chunks<T, 128, even>(c, pl, st);
+  return launch_chunks<T, 256, even>(c, pl, st);
+}
+
+void plan_segments(int B, int kv_heads, int share, int dk, int dv, int T, bool backward, Plan* pl) {
+  const int64_t per_state = backward ? (int64_t)share * slices_of(dk) + slices_of(dk) + slices_of(dv)
+                                     : (int64_t)share * slices_of(dv);
+  split((int64_t)B * kv_heads * per_state, T, &pl->segments, &pl->length);
 }
 
 }  // namespace
 
-size_t linattn_workspace(const zo_linattn&, bool) { return 0; }
+size_t linattn_workspace(const zo_linattn& s, bool backward) {
+  Plan pl{};
+  plan_segments(s.batch, s.kv_heads, s.q_heads / s.kv_heads, s.key_dim, s.value_dim, s.length, backward, &pl);
+  return (size_t)(backward ? 3 : 1) * s.batch * s.kv_heads * (pl.segments - 1) * s.key_dim * s.value_dim *
+         sizeof(float);
+}
 
 hipError_t launch_linattn(const LinCall& c, hipStream_t s) {
   if (c.B == 0) return hipSuccess;
-  return c.dtype == ZO_WBF16 ? launch<uint16_t>(c, s) : launch<float>(c, s);
+  const LinPass& p = c.pass[0];
+  const bool backward = c.npasses > 1;
+  Plan pl{};
+  plan_segments(c.B, c.kv_heads, c.share, backward ? p.dz : p.dx, backward ? p.dx : p.dz, c.T, backward, &pl);
+  bool even = true;
+  int dx = 0;
+  for (int i = 0; i < c.npasses; ++i) {
+    pl.states[i] = (float*)c.work + (int64_t)i * c.B * c.kv_heads * (pl.segments - 1) * p.dx * p.dz;
+    dx = std::max(dx, c.pass[i].dx);
+    const int el = c.dtype == ZO_WBF16 ? 8 : 4;
+    even &= c.pass[i].dx % el == 0 && c.pass[i].dz % el == 0;
+  }
+  if (c.dtype == ZO_WBF16) return even ? launch<uint16_t, true>(c, pl, dx, s) : launch<uint16_t, false>(c, pl, dx, s);
+  return even ? launch<float, true>(c, pl, dx, s) : launch<float, false>(c, pl, dx, s);
 }
 
 }  // namespace zo

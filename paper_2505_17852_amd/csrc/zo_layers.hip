@@ -96,9 +96,8 @@ int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_hea
   p.oh = o->head_stride;
   p.dx = s.key_dim;
   p.dz = s.value_dim;
-  p.out_heads = s.q_heads;
+  p.heads = s.q_heads / s.kv_heads;
   p.sources = 1;
-  p.share = s.q_heads / s.kv_heads;
   p.score = p.carry = s.scale;
   p.upd = 1.0f;
   p.init = initial_state;
@@ -107,6 +106,7 @@ int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_hea
   c.B = s.batch;
   c.T = s.length;
   c.kv_heads = s.kv_heads;
+  c.share = s.q_heads / s.kv_heads;
   c.dtype = s.dtype;
   c.log_decay = log_decay;
   c.lengths = lengths;
@@ -147,9 +147,8 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
   a.oh = dq->head_stride;
   a.dx = s.value_dim;
   a.dz = s.key_dim;
-  a.out_heads = s.q_heads;
+  a.heads = share;
   a.sources = 1;
-  a.share = share;
   a.state_t = 1;
   a.score = a.carry = s.scale;
   a.upd = 1.0f;
@@ -165,9 +164,8 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
   d.oh = dv->head_stride;
   d.dx = s.key_dim;
   d.dz = s.value_dim;
-  d.out_heads = s.kv_heads;
+  d.heads = 1;
   d.sources = share;
-  d.share = 1;
   d.reverse = 1;
   d.score = d.upd = s.scale;
   d.carry = 1.0f;
@@ -191,6 +189,7 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
   c.B = s.batch;
   c.T = s.length;
   c.kv_heads = s.kv_heads;
+  c.share = s.q_heads / s.kv_heads;
   c.dtype = s.dtype;
   c.log_decay = log_decay;
   c.lengths = lengths;

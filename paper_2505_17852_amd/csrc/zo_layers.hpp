@@ -74,9 +74,8 @@ struct LinPass {
   void* out;            // [out heads][dz]
   int64_t ob, ot, oh;
   int dx, dz;
-  int out_heads;        // heads of x and out
-  int sources;          // y/z heads summed into one state (backward: the query heads of a state)
-  int share;            // out heads that read one y/z head (forward: q_heads / kv_heads)
+  int heads;            // out heads per state (forward: the query heads that read it; backward: 1)
+  int sources;          // y/z heads summed into one state (forward: 1; backward: those query heads)
   int reverse;
   int state_t;          // the states' array is [dz][dx] instead of [dx][dz]
   float score, carry, upd;
@@ -87,7 +86,7 @@ constexpr int kLinPasses = 3;
 struct LinCall {
   LinPass pass[kLinPasses];
   int npasses;
-  int B, T, kv_heads;
+  int B, T, kv_heads, share;  // share: query heads per key/value head
   int dtype;
   const float* log_decay;
   const int32_t* lengths;
