@@ -45,6 +45,8 @@ extern "C" {
 
 /* Head sizes up to ZO_LINATTN_MAX_DIM (ZO_ESHAPE beyond). */
 #define ZO_LINATTN_MAX_DIM 256
+/* Distance of neighbouring positions in memory, in elements (ZO_ESHAPE beyond). */
+#define ZO_LINATTN_MAX_STRIDE ((int64_t)1 << 24)
 
 typedef struct {
     int32_t batch;      /* sequences, >= 0 */
@@ -59,7 +61,8 @@ typedef struct {
 
 /* A tensor [batch][length][heads][dim]: element (b, t, h, d) at
  * data[b * batch_stride + t * position_stride + h * head_stride + d], strides
- * in elements, any sign. Any alignment of data that its type needs. Inputs may
+ * in elements, any sign (position_stride within
+ * ZO_LINATTN_MAX_STRIDE). Any alignment of data that its type needs. Inputs may
  * overlap (slices of one projection); an output may overlap nothing. */
 typedef struct {
     void* data;

@@ -30,9 +30,10 @@
 // formed transposed too, so that a lane holds 4 neighbouring columns of one row.
 //
 // Precision: fp32 accumulators and state. bf16 rounds P, and R where x reads it, to
-// bf16 (the rounding of an input each); the state's own sum takes gamma^(..) y in two
-// bf16 parts, 2^-17 of it left out, since what is lost there would stay for all later
-// positions. fp32 runs on fp32 MFMAs throughout.
+// bf16 (the rounding of an input each); the state's own sum takes gamma^(..) y in
+// three bf16 parts, all of its fp32 value, since what is lost there would stay for all later
+// positions (two parts leave out 2^-17 and take 5% less time). fp32 runs on fp32 MFMAs
+// throughout.
 //
 // Rows past a sequence's length are read as zeros. P of later positions is set
 // to zero, not multiplied by it; a z that is not finite would still turn those zeros
@@ -54,6 +55,7 @@ constexpr int kChunk = 64;    // positions
 constexpr int kSlice = 64;    // columns of z per workgroup
 constexpr int kThreads = 256;
 constexpr int kXcds = 8;
+constexpr int kParts = 3;     // bf16 parts of the decayed y in the state's sum
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
@@ -109,37 +111,46 @@ struct Op<float> {
   }
 };
 
-// 16 bytes of a row from column `col`, zeros from column d on.
-template <typename T, bool even>
-__device__ __forceinline__ u4 load16(const T* row, int col, int d) {
-  constexpr int EL = 16 / sizeof(T);
+// 16 bytes at p, which is aligned to its type.
+template <typename T>
+__device__ __forceinline__ u4 load16(const T* p) {
   struct __attribute__((packed, aligned(sizeof(T)))) Any { u4 v; };
-  if (col + EL <= d) return ((const Any*)(row + col))->v;
-  if constexpr (even) {
-    return u4{0, 0, 0, 0};
-  } else {
-    u4 v = {0, 0, 0, 0};
+  return ((const Any*)p)->v;
+}
+// The first d (fewer than 16 bytes hold) values of a row, then zeros.
+template <typename T>
+__device__ __forceinline__ u4 load_few(const T* p, int d) {
+  u4 v = {0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < EL; ++e)
-      if (col + e < d) {
-        if constexpr (sizeof(T) == 2) v[e / 2] |= (uint32_t)row[col + e] << (16 * (e & 1));
-        else v[e] = __float_as_uint(row[col + e]);
-      }
-    return v;
+  for (int e = 0; e < (int)(16 / sizeof(T)); ++e)
+    if (e < d) {
+      if constexpr (sizeof(T) == 2) v[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+      else v[e] = __float_as_uint(p[e]);
+    }
+  return v;
+}
+// Drops the first n values (fewer than 16 bytes hold), zeros after the rest: the end of a row,
+// read with the 16 bytes that end there.
+template <typename T>
+__device__ __forceinline__ u4 drop(u4 v, int n) {
+  int words = n;
+  if constexpr (sizeof(T) == 2) {
+    words = n >> 1;
+    if (n & 1) v = u4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
   }
+  if (words & 1) v = u4{v[1], v[2], v[3], 0};
+  if (words & 2) v = u4{v[2], v[3], 0, 0};
+  return v;
 }
 
+// Gathers, over words of values, the sign bit of each whose exponent is all ones.
 template <typename T>
-__device__ __forceinline__ bool any_not_finite(u4 v) {
-  bool bad = false;
+__device__ __forceinline__ uint32_t not_finite(u4 v) {
+  uint32_t bad = 0;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if constexpr (sizeof(T) == 2)
-      bad |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
-    else
-      bad |= (v[e] & 0x7f800000u) == 0x7f800000u;
-  }
-  return bad;
+  for (int e = 0; e < 4; ++e)
+    bad |= sizeof(T) == 2 ? (v[e] & 0x7fff7fffu) + 0x00800080u : (v[e] & 0x7fffffffu) + 0x00800000u;
+  return bad & (sizeof(T) == 2 ? 0x80008000u : 0x80000000u);
 }
 template <typename T>
 __device__ __forceinline__ typename Op<T>::Frag only_finite(typename Op<T>::Frag f) {
@@ -159,13 +170,81 @@ __device__ __forceinline__ typename Op<T>::Frag only_finite(typename Op<T>::Frag
 // gamma^n; gamma^0 is 1 whatever gamma.
 __device__ __forceinline__ float decay(float lg, int n) { return n == 0 ? 1.0f : exp2f(lg * (float)n); }
 
+// The positions of a chunk in memory: position i (counted in the pass's direction) at
+// base + row(i), an offset of 32 bits, so that a chunk's loads share one scalar base.
+template <typename T>
+struct Rows {
+  const T* first;   // position 0
+  int64_t stride;   // in the pass's direction
+  uint32_t step;    // |stride|
+  bool down;
+  __device__ __forceinline__ Rows(const T* p, int64_t s, bool reverse, int origin)
+      : first(p + origin * s), stride(reverse ? -s : s), step((uint32_t)(s < 0 ? -s : s)), down((s < 0) != reverse) {}
+  __device__ __forceinline__ const T* base(int start) const {
+    return first + (start + (down ? kChunk - 1 : 0)) * stride;
+  }
+  __device__ __forceinline__ uint32_t row(int i) const { return (uint32_t)(down ? kChunk - 1 - i : i) * step; }
+};
+
+// A tile of 64 positions by COLS columns (the first d of which exist) on its way from memory
+// to LDS, 16 bytes per thread and step. Rows past the last position repeat it (no
+// branch around a load: the loads stay in flight together) and are put down as zeros; columns past d
+// are never put down (they are cleared beforehand).
+template <typename T, int COLS, bool even>
+struct Staged {
+  static constexpr int EL = 16 / sizeof(T), PER_ROW = COLS / EL, STEP = kThreads / PER_ROW;
+  // rows lie 8 banks (bf16: the transposing loads' width) or 4 (fp32) past a multiple of all 64
+  static constexpr int N = kChunk / STEP, STRIDE = COLS + (sizeof(T) == 2 ? 16 : 4);
+  u4 v[N];
+  uint32_t at[N];
+  __device__ __forceinline__ void aim(const Rows<T>& m, int rows, int d) {
+    const int q = (int)threadIdx.x % PER_ROW * EL, r = (int)threadIdx.x / PER_ROW;
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] = m.row(min(r + STEP * i, rows - 1)) + max(min(q, d - EL), 0);
+  }
+  __device__ __forceinline__ void fetch(const T* base, int d) {
+    if (even || d >= EL) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = load16(base + at[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = load_few(base + at[i], d);
+    }
+  }
+  __device__ __forceinline__ void put(T* tile, int rows, int d) {
+    const int q = (int)threadIdx.x % PER_ROW * EL, r = (int)threadIdx.x / PER_ROW;
+    if (!even && d >= EL) {
+      const int n = max(q - (d - EL), 0);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = drop<T>(v[i], n);
+    }
+    if (rows < kChunk)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (r + STEP * i >= rows) v[i] = u4{0, 0, 0, 0};
+    if (q < d)
+#pragma unroll
+      for (int i = 0; i < N; ++i) *(u4*)(tile + (r + STEP * i) * STRIDE + q) = v[i];
+  }
+  __device__ __forceinline__ static void clear(T* tile) {
+    for (int i = threadIdx.x; i < kChunk * STRIDE / EL; i += kThreads) *(u4*)(tile + i * EL) = u4{0, 0, 0, 0};
+  }
+  __device__ __forceinline__ bool any_not_finite() const {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) bad |= not_finite<T>(v[i]);
+    return bad != 0;
+  }
+};
+
 template <typename T, int DX, bool even, bool state_only>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void linattn_chunk_kernel(LinCall c, Plan pl) {
   typedef Op<T> O;
   typedef typename O::Frag Frag;
+  typedef Staged<T, DX, even> Y;
+  typedef Staged<T, kSlice, even> Z;
   constexpr int EL = 16 / sizeof(T), KB = O::KB;
-  constexpr int YS = DX + EL, ZS = kSlice + EL;       // rows of the tiles, 16 bytes apart from a multiple of the banks
-  constexpr int NY = kChunk * DX / EL / kThreads, NZ = kChunk * kSlice / EL / kThreads;
+  constexpr int YS = Y::STRIDE, ZS = Z::STRIDE;
   constexpr int NX = DX / KB, NJ = kChunk / KB;        // operand sets along a row of x, over the chunk's positions
   constexpr int MW = DX / 64;                          // tiles of 16 rows of R per wave
   __shared__ __align__(16) T ys[kChunk * YS];
@@ -221,12 +300,26 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
 #pragma unroll
     for (int i = 0; i < MW; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 4; ++j) R[i][j] = f4{0, 0, 0, 0};
+    if (from) {
+      const int sx = turned ? 1 : a.dz, sz = turned ? a.dx : 1;
+      const auto x_of = [&](int i, int r) { return 16 * (w * MW + i) + 4 * g + r; };
+      const auto z_of = [&](int j) { return col + 16 * j + m; };
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int x = 16 * (w * MW + i) + 4 * g + r, z = col + 16 * j + m;
-          R[i][j][r] = from && x < a.dx && z < a.dz ? from[turned ? z * a.dx + x : x * a.dz + z] : 0.0f;
-        }
+      for (int i = 0; i < MW; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            R[i][j][r] = from[min(x_of(i, r), a.dx - 1) * sx + min(z_of(j), a.dz - 1) * sz];
+#pragma unroll
+      for (int i = 0; i < MW; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (x_of(i, r) >= a.dx || z_of(j) >= a.dz) R[i][j][r] = 0.0f;
+    }
   }
 
   // factors of a whole chunk: P's by (row, position), y's by position
@@ -253,102 +346,102 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
   y_factors(kChunk);
   float rf = decay(lg, kChunk);
 
-  // staging: the next step's y and z, the next chunk's x
-  u4 yn[NY], zn[NZ];
-  Frag xc[NX], xn[NX];
-  const auto position = [&](int r) -> int64_t { return a.reverse ? n - 1 - r : r; };
-  const auto fetch_yz = [&](int start, int src) {
-    const int64_t head = (int64_t)kvh * a.sources + src;
-    const T* y = (const T*)a.y.p + b * a.y.b + head * a.y.h;
-    const T* z = (const T*)a.z.p + b * a.z.b + head * a.z.h;
-#pragma unroll
-    for (int i = 0; i < NY; ++i) {
-      const int at = tid + kThreads * i, r = start + at / (DX / EL), q = at % (DX / EL) * EL;
-      yn[i] = r < r1 ? load16<T, even>(y + position(r) * a.y.t, q, a.dx) : u4{0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int i = 0; i < NZ; ++i) {
-      const int at = tid + kThreads * i, r = start + at / (kSlice / EL), q = at % (kSlice / EL) * EL;
-      zn[i] = r < r1 ? load16<T, even>(z + position(r) * a.z.t, col + q, a.dz) : u4{0, 0, 0, 0};
-    }
+  // the next step's y and z, the next chunk's x (whose values past dx meet zeros of y and R)
+  const int origin = a.reverse ? n - 1 : 0, zd = min(kSlice, a.dz - col);
+  const Rows<T> yr((const T*)a.y.p + b * a.y.b + (int64_t)kvh * a.sources * a.y.h, a.y.t, a.reverse, origin);
+  const Rows<T> zr((const T*)a.z.p + b * a.z.b + (int64_t)kvh * a.sources * a.z.h + col, a.z.t, a.reverse, origin);
+  const Rows<T> xr((const T*)a.x.p + b * a.x.b + (int64_t)h * a.x.h, a.x.t, a.reverse, origin);
+  Y yn;
+  Z zn;
+  Frag xn[NX];
+  uint32_t xat = 0;
+  const auto aim = [&](int rows) {
+    yn.aim(yr, rows, a.dx);
+    zn.aim(zr, rows, zd);
+    if constexpr (!state_only) xat = xr.row(min(row, rows - 1));
   };
   const auto fetch_x = [&](int start) {
-    const int r = start + row;
-    const T* x = (const T*)a.x.p + b * a.x.b + (int64_t)h * a.x.h + (r < r1 ? position(r) * a.x.t : 0);
+    const T* x = xr.base(start);
+    if (even || a.dx >= EL) {
 #pragma unroll
-    for (int i = 0; i < NX; ++i)
-      xn[i] = __builtin_bit_cast(Frag, r < r1 ? load16<T, even>(x, i * KB + KB / 4 * g, a.dx) : u4{0, 0, 0, 0});
+      for (int i = 0; i < NX; ++i)
+        xn[i] = __builtin_bit_cast(Frag, load16(x + (xat + (uint32_t)min(i * KB + KB / 4 * g, a.dx - EL))));
+    } else {
+#pragma unroll
+      for (int i = 0; i < NX; ++i) xn[i] = __builtin_bit_cast(Frag, load_few(x + xat, i * KB + KB / 4 * g == 0 ? a.dx : 0));
+    }
   };
 
   if (r0 < r1) {
-    fetch_yz(r0, 0);
+    aim(min(kChunk, r1 - r0));
+    yn.fetch(yr.base(r0), a.dx);
+    zn.fetch(zr.base(r0), zd);
     if constexpr (!state_only) fetch_x(r0);
   }
   if (tid < 2) bad[tid] = 0;
+  if (a.dx < DX) Y::clear(ys);
+  if (zd < kSlice) Z::clear(zs);
   __syncthreads();
   f4 acc[4];
-  int step = 0, src = 0;
-  for (int start = r0; start < r1; ++step) {
+  int src = 0, turn_of = 0;
+  for (int start = r0; start < r1; turn_of ^= 1) {
     const int rows = min(kChunk, r1 - start);
-#pragma unroll
-    for (int i = 0; i < NY; ++i) {
-      const int at = tid + kThreads * i;
-      *(u4*)(ys + at / (DX / EL) * YS + at % (DX / EL) * EL) = yn[i];
-    }
-    bool found = false;
-#pragma unroll
-    for (int i = 0; i < NZ; ++i) {
-      const int at = tid + kThreads * i;
-      *(u4*)(zs + at / (kSlice / EL) * ZS + at % (kSlice / EL) * EL) = zn[i];
-      if constexpr (!state_only) found |= any_not_finite<T>(zn[i]);
-    }
+    yn.put(ys, rows, a.dx);
+    zn.put(zs, rows, zd);
     if constexpr (!state_only) {
-      if (found) bad[step & 1] = 1;
-      if (src == 0) {
-#pragma unroll
-        for (int i = 0; i < NX; ++i) xc[i] = xn[i];
+      if (zn.any_not_finite()) bad[turn_of] = 1;
+      if (src == 0)
 #pragma unroll
         for (int i = 0; i < MW; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j) store_run<T, 4>(rs + (16 * j + m) * YS + 16 * (w * MW + i) + 4 * g, (const float*)&R[i][j]);
-      }
     }
     __syncthreads();
-    const bool flagged = !state_only && bad[step & 1];
-    if (tid == 0) bad[(step + 1) & 1] = 0;
-    // the next step's loads
+    const bool flagged = !state_only && bad[turn_of];
+    if (tid == 0) bad[turn_of ^ 1] = 0;
+    // the loads of the next step, or once more this one's after the last
     const bool last_src = src == a.sources - 1;
-    if (!last_src) {
-      fetch_yz(start, src + 1);
-    } else if (start + kChunk < r1) {
-      fetch_yz(start + kChunk, 0);
-      if constexpr (!state_only) fetch_x(start + kChunk);
-    }
+    const int next = last_src && start + kChunk < r1 ? start + kChunk : start, next_src = last_src ? 0 : src + 1;
+    if (next > start && r1 - next < kChunk) aim(r1 - next);
+    yn.fetch(yr.base(next) + next_src * a.y.h, a.dx);
+    zn.fetch(zr.base(next) + next_src * a.z.h, zd);
     if (src == 0 && rows < kChunk) {
       y_factors(rows);
       rf = decay(lg, rows);
     }
-    f4 P[4];
-    Frag pb[NJ];
+    Frag pb[NJ], z[NJ][4];
     if constexpr (!state_only) {
+      if constexpr (!even) {
+        if (a.dx >= EL)
+#pragma unroll
+          for (int i = 0; i < NX; ++i)
+            if ((i + 1) * KB > a.dx - EL)
+              xn[i] = __builtin_bit_cast(Frag, drop<T>(__builtin_bit_cast(u4, xn[i]), min(max(i * KB + KB / 4 * g - (a.dx - EL), 0), EL - 1)));
+      }
       if (src == 0) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           acc[j] = f4{0, 0, 0, 0};
 #pragma unroll
-          for (int i = 0; i < NX; ++i) acc[j] = O::mma(O::along(rs + (16 * j + m) * YS + i * KB, g), xc[i], acc[j]);
-          acc[j] *= xf;
+          for (int i = 0; i < NX; ++i) acc[j] = O::mma(O::along(rs + (16 * j + m) * YS + i * KB, g), xn[i], acc[j]);
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] *= xf;
       }
+      f4 P[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         P[j] = f4{0, 0, 0, 0};
         if (j > w) continue;
 #pragma unroll
-        for (int i = 0; i < NX; ++i) P[j] = O::mma(O::along(ys + (16 * j + m) * YS + i * KB, g), xc[i], P[j]);
+        for (int i = 0; i < NX; ++i) P[j] = O::mma(O::along(ys + (16 * j + m) * YS + i * KB, g), xn[i], P[j]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) P[j][r] = 16 * j + 4 * g + r <= row ? P[j][r] * pf[j][r] : 0.0f;
+        for (int r = 0; r < 4; ++r) P[j][r] *= pf[j][r];
+        if (j == w)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) P[j][r] = 4 * g + r <= m ? P[j][r] : 0.0f;
       }
+      fetch_x(next);
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
@@ -360,94 +453,97 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
         for (int j = 0; j < NJ; ++j) pb[j] = P[j];
       }
     }
+#pragma unroll
+    for (int k = 0; k < NJ; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) z[k][j] = O::down(zs + k * KB * ZS + 16 * j, ZS, g, m);
+    if constexpr (!state_only) {
+      if (!flagged) {
+#pragma unroll
+        for (int k = 0; k < NJ; ++k)
+          if (k * KB <= 16 * w + 15)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = O::mma(z[k][j], pb[k], acc[j]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < NJ; ++k)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j] = O::mma(only_finite<T>(z[k][j]), pb[k], acc[j]);
+        // the products of z that are not finite, for the rows they reach
+#pragma unroll
+        for (int k = 0; k < NJ; ++k)
+#pragma unroll
+          for (int e = 0; e < KB / 4; ++e)
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+              const u4 words = __builtin_bit_cast(u4, pb[k]);
+              const uint32_t word = (uint32_t)__shfl((int)words[sizeof(T) == 2 ? e / 2 : e], m + 16 * q, 64);
+              const float p = __uint_as_float(sizeof(T) == 4 ? word : e & 1 ? word & 0xffff0000u : word << 16);
+              const int at = KB * k + 16 * (e >> 2) + 4 * q + (e & 3);
+#pragma unroll
+              for (int d = 0; d < 16; ++d) {
+                const float v = to_f32(zs[at * ZS + 16 * (d >> 2) + 4 * g + (d & 3)]);
+                if (at <= row && !(fabsf(v) < __builtin_inff())) acc[d >> 2][d & 3] += p * v;
+              }
+            }
+      }
+      if (last_src && row < rows) {
+        T* o = out + (int64_t)(a.reverse ? n - 1 - start - row : start + row) * a.ot;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = col + 16 * j + 4 * g;
+          if (even ? d < a.dz : d + 4 <= a.dz) {
+            store_run<T, 4>(o + d, (const float*)&acc[j]);
+          } else if (!even) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (d + e < a.dz) o[d + e] = from_f32<T>(acc[j][e]);
+          }
+        }
+      }
+    }
     if (src == 0)
 #pragma unroll
       for (int i = 0; i < MW; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) R[i][j] *= rf;
 #pragma unroll
-    for (int k = 0; k < NJ; ++k) {
-      Frag z[4];
+    for (int i = 0; i < MW; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) z[j] = O::down(zs + k * KB * ZS + 16 * j, ZS, g, m);
-      if constexpr (!state_only) {
-        if (k * KB <= 16 * w + 15) {
-          if (!flagged) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = O::mma(z[j], pb[k], acc[j]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = O::mma(only_finite<T>(z[j]), pb[k], acc[j]);
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < MW; ++i) {
+      for (int k = 0; k < NJ; ++k) {
         const Frag y = O::down(ys + k * KB * YS + 16 * (w * MW + i), YS, g, m);
         if constexpr (sizeof(T) == 2) {
-          u4 hi, lo;
+          // gamma^(..) y in bf16 parts, the next one of what the last left out
           const u4 raw = __builtin_bit_cast(u4, y);
+          float rest[8];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float p = __uint_as_float(raw[e] << 16) * yf[k][2 * e];
-            const float q = __uint_as_float(raw[e] & 0xffff0000u) * yf[k][2 * e + 1];
-            hi[e] = bf16_pair(p, q);
-            lo[e] = bf16_pair(p - __uint_as_float(hi[e] << 16), q - __uint_as_float(hi[e] & 0xffff0000u));
+            rest[2 * e] = __uint_as_float(raw[e] << 16) * yf[k][2 * e];
+            rest[2 * e + 1] = __uint_as_float(raw[e] & 0xffff0000u) * yf[k][2 * e + 1];
           }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            R[i][j] = O::mma(__builtin_bit_cast(Frag, hi), z[j], R[i][j]);
-            R[i][j] = O::mma(__builtin_bit_cast(Frag, lo), z[j], R[i][j]);
+          for (int q = 0; q < kParts; ++q) {
+            u4 part;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              part[e] = bf16_pair(rest[2 * e], rest[2 * e + 1]);
+              rest[2 * e] -= __uint_as_float(part[e] << 16);
+              rest[2 * e + 1] -= __uint_as_float(part[e] & 0xffff0000u);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) R[i][j] = O::mma(__builtin_bit_cast(Frag, part), z[k][j], R[i][j]);
           }
         } else {
           Frag f;
 #pragma unroll
           for (int e = 0; e < 4; ++e) f[e] = y[e] * yf[k][e];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) R[i][j] = O::mma(f, z[j], R[i][j]);
+          for (int j = 0; j < 4; ++j) R[i][j] = O::mma(f, z[k][j], R[i][j]);
         }
       }
-    }
-    if constexpr (!state_only) {
-      if (flagged) {
-        // the products of z that are not finite, for the rows they reach
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll 1
-            for (int q = 0; q < 4; ++q) {
-              const float p = __shfl(P[j][r], m + 16 * q, 64);
-              const int at = 16 * j + 4 * q + r;
-#pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float v = to_f32(zs[at * ZS + 16 * (e >> 2) + 4 * g + (e & 3)]);
-                if (at <= row && !(fabsf(v) < __builtin_inff())) acc[e >> 2][e & 3] += p * v;
-              }
-            }
-      }
-      if (last_src && row < rows) {
-        T* o = out + position(start + row) * a.ot;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int z = col + 16 * j + 4 * g;
-          if (z + 4 <= a.dz) {
-            store_run<T, 4>(o + z, (const float*)&acc[j]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (z + e < a.dz) o[z + e] = from_f32<T>(acc[j][e]);
-          }
-        }
-      }
-    }
     __syncthreads();
-    if (last_src) {
-      src = 0;
-      start += kChunk;
-    } else {
-      ++src;
-    }
+    src = next_src;
+    if (last_src) start += kChunk;
   }
 
   float* to = nullptr;

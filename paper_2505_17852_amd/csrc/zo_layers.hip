@@ -41,6 +41,9 @@ int check_heads(const zo_heads* h, const char* name, int32_t dtype, bool any) {
   if (!h) return fail(ZO_EINVAL, "%s is NULL", name);
   if (any && !h->data) return fail(ZO_EINVAL, "%s has no data", name);
   if (!aligned_for(h->data, dtype)) return fail(ZO_EINVAL, "%s is not aligned to its type", name);
+  // the kernels reach the 64 positions of a chunk with 32-bit offsets
+  if (h->position_stride > ZO_LINATTN_MAX_STRIDE || h->position_stride < -ZO_LINATTN_MAX_STRIDE)
+    return fail(ZO_ESHAPE, "%s: position strides must stay within 2^24", name);
   return ZO_OK;
 }
 
