@@ -18,7 +18,7 @@
 // one sequence, head and slice of 64 columns of z with R in its accumulators:
 // x, y, z are read and out is written once per slice (the slices and passes of a
 // state run next to each other on one XCD, whose L2 serves the second reading).
-// Wave w has the chunk's rows 16 w .. 16 w + 15 and a quarter of R's rows.
+// Wave w has the chunk's rows 16 w .. 16 w + 15 and 16 of R's columns.
 //
 // Operands. MFMA 16x16: A and B have the same lane layout, lane l = row (or column)
 // l % 16, contraction index group l / 16; the result has column l % 16 and
@@ -30,12 +30,12 @@
 // formed transposed too, so that a lane holds 4 neighbouring columns of one row.
 //
 // Precision: fp32 accumulators and state. bf16 rounds P, and R where x reads it, to
-// bf16 (the rounding of an input each); the state's own sum takes gamma^(..) y in
+// bf16 (the rounding of an input each); the state's own sum takes gamma^(..) z in
 // three bf16 parts, all of its fp32 value, since what is lost there would stay for all later
 // positions (two parts leave out 2^-17 and take 5% less time). fp32 runs on fp32 MFMAs
 // throughout.
 //
-// Rows past a sequence's length are read as zeros. P of later positions is set
+// Positions past a sequence's length are never read. P of later positions is set
 // to zero, not multiplied by it; a z that is not finite would still turn those zeros
 // into NaN, so chunks that hold one (seen when it is staged) take z without it
 // and add its products to the rows that it reaches.
@@ -55,7 +55,7 @@ constexpr int kChunk = 64;    // positions
 constexpr int kSlice = 64;    // columns of z per workgroup
 constexpr int kThreads = 256;
 constexpr int kXcds = 8;
-constexpr int kParts = 3;     // bf16 parts of the decayed y in the state's sum
+constexpr int kParts = 3;     // bf16 parts of the decayed z in the state's sum
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
@@ -187,9 +187,9 @@ struct Rows {
 };
 
 // A tile of 64 positions by COLS columns (the first d of which exist) on its way from memory
-// to LDS, 16 bytes per thread and step. Rows past the last position repeat it (no
-// branch around a load: the loads stay in flight together) and are put down as zeros; columns past d
-// are never put down (they are cleared beforehand).
+// to LDS, 16 bytes per thread and step. Rows before the first position (`lead` of them)
+// repeat it (no branch around a load: the loads stay in flight together) and are put down as
+// zeros; columns past d are never put down (they are cleared beforehand).
 template <typename T, int COLS, bool even>
 struct Staged {
   static constexpr int EL = 16 / sizeof(T), PER_ROW = COLS / EL, STEP = kThreads / PER_ROW;
@@ -197,10 +197,10 @@ struct Staged {
   static constexpr int N = kChunk / STEP, STRIDE = COLS + (sizeof(T) == 2 ? 16 : 4);
   u4 v[N];
   uint32_t at[N];
-  __device__ __forceinline__ void aim(const Rows<T>& m, int rows, int d) {
+  __device__ __forceinline__ void aim(const Rows<T>& m, int lead, int d) {
     const int q = (int)threadIdx.x % PER_ROW * EL, r = (int)threadIdx.x / PER_ROW;
 #pragma unroll
-    for (int i = 0; i < N; ++i) at[i] = m.row(min(r + STEP * i, rows - 1)) + max(min(q, d - EL), 0);
+    for (int i = 0; i < N; ++i) at[i] = m.row(max(r + STEP * i, lead)) + max(min(q, d - EL), 0);
   }
   __device__ __forceinline__ void fetch(const T* base, int d) {
     if (even || d >= EL) {
@@ -211,17 +211,17 @@ struct Staged {
       for (int i = 0; i < N; ++i) v[i] = load_few(base + at[i], d);
     }
   }
-  __device__ __forceinline__ void put(T* tile, int rows, int d) {
+  __device__ __forceinline__ void put(T* tile, int lead, int d) {
     const int q = (int)threadIdx.x % PER_ROW * EL, r = (int)threadIdx.x / PER_ROW;
     if (!even && d >= EL) {
       const int n = max(q - (d - EL), 0);
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] = drop<T>(v[i], n);
     }
-    if (rows < kChunk)
+    if (lead)
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        if (r + STEP * i >= rows) v[i] = u4{0, 0, 0, 0};
+        if (r + STEP * i < lead) v[i] = u4{0, 0, 0, 0};
     if (q < d)
 #pragma unroll
       for (int i = 0; i < N; ++i) *(u4*)(tile + (r + STEP * i) * STRIDE + q) = v[i];
@@ -238,7 +238,7 @@ struct Staged {
 };
 
 template <typename T, int DX, bool even, bool state_only>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void linattn_chunk_kernel(LinCall c, Plan pl) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 2 : 1) void linattn_chunk_kernel(LinCall c, Plan pl) {
   typedef Op<T> O;
   typedef typename O::Frag Frag;
   typedef Staged<T, DX, even> Y;
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
   constexpr int EL = 16 / sizeof(T), KB = O::KB;
   constexpr int YS = Y::STRIDE, ZS = Z::STRIDE;
   constexpr int NX = DX / KB, NJ = kChunk / KB;        // operand sets along a row of x, over the chunk's positions
-  constexpr int MW = DX / 64;                          // tiles of 16 rows of R per wave
+  constexpr int MT = DX / 16;                          // tiles of 16 rows of R
   __shared__ __align__(16) T ys[kChunk * YS];
   __shared__ __align__(16) T zs[kChunk * ZS];
   __shared__ __align__(16) T rs[state_only ? 1 : kSlice * YS];  // R^T where x reads it
@@ -286,8 +286,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
     if (r0 >= n && seg > 0) return;
   }
 
-  // R: rows 16 (w MW + i) + 4 g + r, columns col + 16 j + m
-  f4 R[MW][4];
+  // R: rows 16 i + 4 g + r, column col + 16 w + m
+  f4 R[MT];
+  const int rz = col + 16 * w + m;
   {
     const float* from = nullptr;
     bool turned = false;
@@ -298,33 +299,26 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
       from = pl.states[pass] + (bh * (pl.segments - 1) + seg - 1) * a.dx * a.dz;
     }
 #pragma unroll
-    for (int i = 0; i < MW; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) R[i][j] = f4{0, 0, 0, 0};
+    for (int i = 0; i < MT; ++i) R[i] = f4{0, 0, 0, 0};
     if (from) {
       const int sx = turned ? 1 : a.dz, sz = turned ? a.dx : 1;
-      const auto x_of = [&](int i, int r) { return 16 * (w * MW + i) + 4 * g + r; };
-      const auto z_of = [&](int j) { return col + 16 * j + m; };
 #pragma unroll
-      for (int i = 0; i < MW; ++i)
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int r = 0; r < 4; ++r) R[i][r] = from[min(16 * i + 4 * g + r, a.dx - 1) * sx + min(rz, a.dz - 1) * sz];
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            R[i][j][r] = from[min(x_of(i, r), a.dx - 1) * sx + min(z_of(j), a.dz - 1) * sz];
+      for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int i = 0; i < MW; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (x_of(i, r) >= a.dx || z_of(j) >= a.dz) R[i][j][r] = 0.0f;
+        for (int r = 0; r < 4; ++r)
+          if (16 * i + 4 * g + r >= a.dx || rz >= a.dz) R[i][r] = 0.0f;
     }
   }
 
-  // factors of a whole chunk: P's by (row, position), y's by position
+  // factors: P's by (row, position), z's by position. The first chunk may begin before the segment, by
+  // `lead` rows of zeros, so that all others are whole and these never change.
   const int row = 16 * w + m;
-  float pf[4][4], yf[NJ][KB / 4];
+  const int lead0 = (kChunk - (r1 - r0) % kChunk) % kChunk;
+  float pf[4][4], zf[NJ][KB / 4];
   if constexpr (!state_only)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -333,18 +327,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
         const int apart = row - (16 * j + 4 * g + r);
         pf[j][r] = apart >= 0 ? a.score * decay(lg, apart) : 0.0f;
       }
-  const float xf = state_only ? 0.0f : a.carry * decay(lg, row + off);
-  const auto y_factors = [&](int rows) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
+  for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int e = 0; e < KB / 4; ++e) {
-        const int at = KB * j + 16 * (e >> 2) + 4 * g + (e & 3);
-        yf[j][e] = at < rows ? a.upd * decay(lg, rows - off - at) : 0.0f;
-      }
-  };
-  y_factors(kChunk);
-  float rf = decay(lg, kChunk);
+    for (int e = 0; e < KB / 4; ++e)
+      zf[j][e] = a.upd * decay(lg, kChunk - off - (KB * j + 16 * (e >> 2) + 4 * g + (e & 3)));
+  // of the carried state: what reaches a row, and what is left after the chunk
+  float xf = a.carry * decay(lg, max(row - lead0, 0) + off), rf = decay(lg, kChunk - lead0);
 
   // the next step's y and z, the next chunk's x (whose values past dx meet zeros of y and R)
   const int origin = a.reverse ? n - 1 : 0, zd = min(kSlice, a.dz - col);
@@ -355,10 +344,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
   Z zn;
   Frag xn[NX];
   uint32_t xat = 0;
-  const auto aim = [&](int rows) {
-    yn.aim(yr, rows, a.dx);
-    zn.aim(zr, rows, zd);
-    if constexpr (!state_only) xat = xr.row(min(row, rows - 1));
+  const auto aim = [&](int lead) {
+    yn.aim(yr, lead, a.dx);
+    zn.aim(zr, lead, zd);
+    if constexpr (!state_only) xat = xr.row(max(row, lead));
   };
   const auto fetch_x = [&](int start) {
     const T* x = xr.base(start);
@@ -373,10 +362,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
   };
 
   if (r0 < r1) {
-    aim(min(kChunk, r1 - r0));
-    yn.fetch(yr.base(r0), a.dx);
-    zn.fetch(zr.base(r0), zd);
-    if constexpr (!state_only) fetch_x(r0);
+    aim(lead0);
+    yn.fetch(yr.base(r0 - lead0), a.dx);
+    zn.fetch(zr.base(r0 - lead0), zd);
+    if constexpr (!state_only) fetch_x(r0 - lead0);
   }
   if (tid < 2) bad[tid] = 0;
   if (a.dx < DX) Y::clear(ys);
@@ -384,17 +373,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
   __syncthreads();
   f4 acc[4];
   int src = 0, turn_of = 0;
-  for (int start = r0; start < r1; turn_of ^= 1) {
-    const int rows = min(kChunk, r1 - start);
-    yn.put(ys, rows, a.dx);
-    zn.put(zs, rows, zd);
+  for (int start = r0 - lead0; start < r1; turn_of ^= 1) {
+    const int lead = max(r0 - start, 0);
+    yn.put(ys, lead, a.dx);
+    zn.put(zs, lead, zd);
     if constexpr (!state_only) {
       if (zn.any_not_finite()) bad[turn_of] = 1;
       if (src == 0)
 #pragma unroll
-        for (int i = 0; i < MW; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) store_run<T, 4>(rs + (16 * j + m) * YS + 16 * (w * MW + i) + 4 * g, (const float*)&R[i][j]);
+        for (int i = 0; i < MT; ++i) store_run<T, 4>(rs + (16 * w + m) * YS + 16 * i + 4 * g, (const float*)&R[i]);
     }
     __syncthreads();
     const bool flagged = !state_only && bad[turn_of];
@@ -402,14 +389,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
     // the loads of the next step, or once more this one's after the last
     const bool last_src = src == a.sources - 1;
     const int next = last_src && start + kChunk < r1 ? start + kChunk : start, next_src = last_src ? 0 : src + 1;
-    if (next > start && r1 - next < kChunk) aim(r1 - next);
+    if (next > start && lead) aim(0);
     yn.fetch(yr.base(next) + next_src * a.y.h, a.dx);
     zn.fetch(zr.base(next) + next_src * a.z.h, zd);
-    if (src == 0 && rows < kChunk) {
-      y_factors(rows);
-      rf = decay(lg, rows);
-    }
-    Frag pb[NJ], z[NJ][4];
+    Frag pb[NJ];
     if constexpr (!state_only) {
       if constexpr (!even) {
         if (a.dx >= EL)
@@ -453,41 +436,39 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
         for (int j = 0; j < NJ; ++j) pb[j] = P[j];
       }
     }
-#pragma unroll
-    for (int k = 0; k < NJ; ++k)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) z[k][j] = O::down(zs + k * KB * ZS + 16 * j, ZS, g, m);
     if constexpr (!state_only) {
       if (!flagged) {
 #pragma unroll
         for (int k = 0; k < NJ; ++k)
           if (k * KB <= 16 * w + 15)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = O::mma(z[k][j], pb[k], acc[j]);
+            for (int j = 0; j < 4; ++j) acc[j] = O::mma(O::down(zs + k * KB * ZS + 16 * j, ZS, g, m), pb[k], acc[j]);
       } else {
 #pragma unroll
         for (int k = 0; k < NJ; ++k)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[j] = O::mma(only_finite<T>(z[k][j]), pb[k], acc[j]);
+          for (int j = 0; j < 4; ++j) acc[j] = O::mma(only_finite<T>(O::down(zs + k * KB * ZS + 16 * j, ZS, g, m)), pb[k], acc[j]);
         // the products of z that are not finite, for the rows they reach
-#pragma unroll
-        for (int k = 0; k < NJ; ++k)
-#pragma unroll
-          for (int e = 0; e < KB / 4; ++e)
+        constexpr int WORDS = 4 * NJ;
+        int zat = 4 * g;
+        asm volatile("" : "+v"(zat));  // (keeps this path's addresses out of the others' registers)
 #pragma unroll 1
-            for (int q = 0; q < 4; ++q) {
-              const u4 words = __builtin_bit_cast(u4, pb[k]);
-              const uint32_t word = (uint32_t)__shfl((int)words[sizeof(T) == 2 ? e / 2 : e], m + 16 * q, 64);
-              const float p = __uint_as_float(sizeof(T) == 4 ? word : e & 1 ? word & 0xffff0000u : word << 16);
-              const int at = KB * k + 16 * (e >> 2) + 4 * q + (e & 3);
+        for (int at = 0; at < kChunk; ++at) {
+          // P of position at: in lanes of group (at / 4) % 4, values 4 (at / 16) + at % 4 of the operands
+          const int value = (at >> 4) * 4 + (at & 3), want = sizeof(T) == 2 ? value >> 1 : value;
+          uint32_t word = 0;
 #pragma unroll
-              for (int d = 0; d < 16; ++d) {
-                const float v = to_f32(zs[at * ZS + 16 * (d >> 2) + 4 * g + (d & 3)]);
-                if (at <= row && !(fabsf(v) < __builtin_inff())) acc[d >> 2][d & 3] += p * v;
-              }
-            }
+          for (int e = 0; e < WORDS; ++e) word = e == want ? __builtin_bit_cast(u4, pb[e >> 2])[e & 3] : word;
+          word = (uint32_t)__shfl((int)word, m + 16 * ((at >> 2) & 3), 64);
+          const float p = __uint_as_float(sizeof(T) == 4 ? word : at & 1 ? word & 0xffff0000u : word << 16);
+#pragma unroll
+          for (int d = 0; d < 16; ++d) {
+            const float v = to_f32(zs[at * ZS + zat + 16 * (d >> 2) + (d & 3)]);
+            if (at <= row && !(fabsf(v) < __builtin_inff())) acc[d >> 2][d & 3] += p * v;
+          }
+        }
       }
-      if (last_src && row < rows) {
+      if (last_src && row >= lead) {
         T* o = out + (int64_t)(a.reverse ? n - 1 - start - row : start + row) * a.ot;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -504,46 +485,51 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
     }
     if (src == 0)
 #pragma unroll
-      for (int i = 0; i < MW; ++i)
+      for (int i = 0; i < MT; ++i) R[i] *= rf;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) R[i][j] *= rf;
+    for (int k = 0; k < NJ; ++k) {
+      const Frag own = O::down(zs + k * KB * ZS + 16 * w, ZS, g, m);
+      if constexpr (sizeof(T) == 2) {
+        // gamma^(..) z in bf16 parts, the next one of what the last left out
+        const u4 raw = __builtin_bit_cast(u4, own);
+        float rest[8];
+        u4 part[kParts];
 #pragma unroll
-    for (int i = 0; i < MW; ++i)
+        for (int e = 0; e < 4; ++e) {
+          rest[2 * e] = __uint_as_float(raw[e] << 16) * zf[k][2 * e];
+          rest[2 * e + 1] = __uint_as_float(raw[e] & 0xffff0000u) * zf[k][2 * e + 1];
+        }
 #pragma unroll
-      for (int k = 0; k < NJ; ++k) {
-        const Frag y = O::down(ys + k * KB * YS + 16 * (w * MW + i), YS, g, m);
-        if constexpr (sizeof(T) == 2) {
-          // gamma^(..) y in bf16 parts, the next one of what the last left out
-          const u4 raw = __builtin_bit_cast(u4, y);
-          float rest[8];
+        for (int q = 0; q < kParts; ++q)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            rest[2 * e] = __uint_as_float(raw[e] << 16) * yf[k][2 * e];
-            rest[2 * e + 1] = __uint_as_float(raw[e] & 0xffff0000u) * yf[k][2 * e + 1];
+            part[q][e] = bf16_pair(rest[2 * e], rest[2 * e + 1]);
+            rest[2 * e] -= __uint_as_float(part[q][e] << 16);
+            rest[2 * e + 1] -= __uint_as_float(part[q][e] & 0xffff0000u);
           }
 #pragma unroll
-          for (int q = 0; q < kParts; ++q) {
-            u4 part;
+        for (int i = 0; i < MT; ++i) {
+          const Frag y = O::down(ys + k * KB * YS + 16 * i, YS, g, m);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              part[e] = bf16_pair(rest[2 * e], rest[2 * e + 1]);
-              rest[2 * e] -= __uint_as_float(part[e] << 16);
-              rest[2 * e + 1] -= __uint_as_float(part[e] & 0xffff0000u);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) R[i][j] = O::mma(__builtin_bit_cast(Frag, part), z[k][j], R[i][j]);
-          }
-        } else {
-          Frag f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) f[e] = y[e] * yf[k][e];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) R[i][j] = O::mma(f, z[k][j], R[i][j]);
+          for (int q = 0; q < kParts; ++q) R[i] = O::mma(y, __builtin_bit_cast(Frag, part[q]), R[i]);
         }
+      } else {
+        Frag f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = own[e] * zf[k][e];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) R[i] = O::mma(O::down(ys + k * KB * YS + 16 * i, YS, g, m), f, R[i]);
       }
+    }
     __syncthreads();
     src = next_src;
-    if (last_src) start += kChunk;
+    if (last_src) {
+      if (lead) {
+        xf = a.carry * decay(lg, row + off);
+        rf = decay(lg, kChunk);
+      }
+      start += kChunk;
+    }
   }
 
   float* to = nullptr;
@@ -554,16 +540,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX < 256 ? 2 : 1) void 
     to = a.fin + bh * a.dx * a.dz;
     turned = a.state_t;
   }
-  if (to)
+  if (to && rz < a.dz)
 #pragma unroll
-    for (int i = 0; i < MW; ++i)
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int x = 16 * (w * MW + i) + 4 * g + r, z = col + 16 * j + m;
-          if (x < a.dx && z < a.dz) to[turned ? z * a.dx + x : x * a.dz + z] = R[i][j][r];
-        }
+      for (int r = 0; r < 4; ++r) {
+        const int x = 16 * i + 4 * g + r;
+        if (x < a.dx) to[turned ? rz * a.dx + x : x * a.dz + rz] = R[i][r];
+      }
 }
 
 // Adds up the segments' states: state_s = gamma^length state_(s-1) + its own sum.
