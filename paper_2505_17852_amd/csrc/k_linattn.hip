@@ -84,12 +84,13 @@ struct Op<uint16_t> {
   }
   // contraction along a row: 8 values from index 8 g
   static __device__ __forceinline__ Frag along(const uint16_t* row, int g) { return *(const Frag*)(row + 8 * g); }
-  // contraction over rows: rows 4 g .. 4 g + 3 and 16 + 4 g .., column l % 16
-  static __device__ __forceinline__ Frag down(const uint16_t* tile, int stride, int g, int m) {
+  // contraction over rows: rows 4 g .. 4 g + 3 of each of two tiles of 16 rows, column l % 16
+  static constexpr int TILES = 2;
+  static __device__ __forceinline__ Frag down(const uint16_t* tile0, const uint16_t* tile1, int stride, int g, int m) {
     typedef __attribute__((address_space(3))) s4 Lds;
-    const uint16_t* p = tile + (4 * g + (m >> 2)) * stride + 4 * (m & 3);
-    const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)p);
-    const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(p + 16 * stride));
+    const int at = (4 * g + (m >> 2)) * stride + 4 * (m & 3);
+    const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(tile0 + at));
+    const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(tile1 + at));
     return __builtin_bit_cast(Frag, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
@@ -103,7 +104,8 @@ struct Op<float> {
     return c;
   }
   static __device__ __forceinline__ Frag along(const float* row, int g) { return *(const Frag*)(row + 4 * g); }
-  static __device__ __forceinline__ Frag down(const float* tile, int stride, int g, int m) {
+  static constexpr int TILES = 1;
+  static __device__ __forceinline__ Frag down(const float* tile, const float*, int stride, int g, int m) {
     Frag f;
 #pragma unroll
     for (int s = 0; s < 4; ++s) f[s] = tile[(4 * g + s) * stride + m];
@@ -237,6 +239,41 @@ struct Staged {
   }
 };
 
+// Stores a wave's 16 rows of 64 columns (d of which exist): lane l holds columns 16 j + 4 (l / 16) .. of row l % 16.
+// bf16: lanes of neighbouring groups swap halves, so that each stores 16 bytes and a row 64 in one instruction.
+template <typename T, bool even>
+__device__ __forceinline__ void store_rows(const f4 (&acc)[4], T* row, bool exists, int d, int g) {
+  if constexpr (sizeof(T) == 2 && even) {
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+      u4 v;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const auto s = __builtin_amdgcn_permlane16_swap(bf16_pair(acc[j][2 * e], acc[j][2 * e + 1]),
+                                                        bf16_pair(acc[j + 1][2 * e], acc[j + 1][2 * e + 1]), false, false);
+        v[e] = s[0];
+        v[2 + e] = s[1];
+      }
+      // groups 0 and 2 now hold columns 0 .. 7 and 8 .. 15 of tile j, groups 1 and 3 of tile j + 1
+      const int at = 16 * j + 16 * (g & 1) + 4 * (g & 2);
+      struct __attribute__((packed, aligned(sizeof(T)))) Any { u4 v; };
+      if (exists && at < d) ((Any*)(row + at))->v = v;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int at = 16 * j + 4 * g;
+      if (exists && (even ? at < d : at + 4 <= d)) {
+        store_run<T, 4>(row + at, (const float*)&acc[j]);
+      } else if (!even && exists) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (at + e < d) row[at + e] = from_f32<T>(acc[j][e]);
+      }
+    }
+  }
+}
+
 template <typename T, int DX, bool even, bool state_only>
 __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 2 : 1) void linattn_chunk_kernel(LinCall c, Plan pl) {
   typedef Op<T> O;
@@ -314,24 +351,22 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
     }
   }
 
-  // factors: P's by (row, position), z's by position. The first chunk may begin before the segment, by
+  // Factors of the scores and of z. The first chunk may begin before the segment, by
   // `lead` rows of zeros, so that all others are whole and these never change.
   const int row = 16 * w + m;
   const int lead0 = (kChunk - (r1 - r0) % kChunk) % kChunk;
-  float pf[4][4], zf[NJ][KB / 4];
-  if constexpr (!state_only)
+  // Scores go by tiles of 16 positions backwards from the wave's own: tile t holds positions 16 (w - t) .., all of
+  // them before the rows for t >= 1 (none at all for t > w). Each factor is a product of two powers, both of
+  // exponents >= 0 (no overflow however strong the decay), one by lane and one by tile.
+  float own_f[4], far_f[4], pos_f[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int apart = row - (16 * j + 4 * g + r);
-        pf[j][r] = apart >= 0 ? a.score * decay(lg, apart) : 0.0f;
-      }
-#pragma unroll
-  for (int j = 0; j < NJ; ++j)
-#pragma unroll
-    for (int e = 0; e < KB / 4; ++e)
-      zf[j][e] = a.upd * decay(lg, kChunk - off - (KB * j + 16 * (e >> 2) + 4 * g + (e & 3)));
+  for (int r = 0; r < 4; ++r) {
+    const int apart = m - 4 * g - r;
+    own_f[r] = state_only ? 0.0f : a.score * decay(lg, max(apart, 0));
+    far_f[r] = state_only ? 0.0f : a.score * decay(lg, apart + 16);
+    pos_f[r] = a.upd * decay(lg, 16 - off - 4 * g - r);
+  }
+  const float tile_f[4] = {1.0f, decay(lg, 16), decay(lg, 32), decay(lg, 48)};
   // of the carried state: what reaches a row, and what is left after the chunk
   float xf = a.carry * decay(lg, max(row - lead0, 0) + off), rf = decay(lg, kChunk - lead0);
 
@@ -340,6 +375,11 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   const Rows<T> yr((const T*)a.y.p + b * a.y.b + (int64_t)kvh * a.sources * a.y.h, a.y.t, a.reverse, origin);
   const Rows<T> zr((const T*)a.z.p + b * a.z.b + (int64_t)kvh * a.sources * a.z.h + col, a.z.t, a.reverse, origin);
   const Rows<T> xr((const T*)a.x.p + b * a.x.b + (int64_t)h * a.x.h, a.x.t, a.reverse, origin);
+  // (kept in scalar registers: loads of arguments inside the loop would wait for the LDS too)
+  int64_t yh = a.y.h, zh = a.z.h, out_turn = a.reverse ? -a.ot : a.ot;
+  T* outp = out + origin * a.ot + col;
+  int sources = a.sources, dxn = a.dx;
+  asm volatile("" : "+s"(yh), "+s"(zh), "+s"(out_turn), "+s"(outp), "+s"(sources), "+s"(dxn));
   Y yn;
   Z zn;
   Frag xn[NX];
@@ -351,10 +391,10 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   };
   const auto fetch_x = [&](int start) {
     const T* x = xr.base(start);
-    if (even || a.dx >= EL) {
+    if (even || dxn >= EL) {
 #pragma unroll
       for (int i = 0; i < NX; ++i)
-        xn[i] = __builtin_bit_cast(Frag, load16(x + (xat + (uint32_t)min(i * KB + KB / 4 * g, a.dx - EL))));
+        xn[i] = __builtin_bit_cast(Frag, load16(x + (xat + (uint32_t)min(i * KB + KB / 4 * g, dxn - EL))));
     } else {
 #pragma unroll
       for (int i = 0; i < NX; ++i) xn[i] = __builtin_bit_cast(Frag, load_few(x + xat, i * KB + KB / 4 * g == 0 ? a.dx : 0));
@@ -375,7 +415,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   int src = 0, turn_of = 0;
   for (int start = r0 - lead0; start < r1; turn_of ^= 1) {
     const int lead = max(r0 - start, 0);
-    yn.put(ys, lead, a.dx);
+    yn.put(ys, lead, dxn);
     zn.put(zs, lead, zd);
     if constexpr (!state_only) {
       if (zn.any_not_finite()) bad[turn_of] = 1;
@@ -387,12 +427,13 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
     const bool flagged = !state_only && bad[turn_of];
     if (tid == 0) bad[turn_of ^ 1] = 0;
     // the loads of the next step, or once more this one's after the last
-    const bool last_src = src == a.sources - 1;
+    const bool last_src = src == sources - 1;
     const int next = last_src && start + kChunk < r1 ? start + kChunk : start, next_src = last_src ? 0 : src + 1;
     if (next > start && lead) aim(0);
-    yn.fetch(yr.base(next) + next_src * a.y.h, a.dx);
-    zn.fetch(zr.base(next) + next_src * a.z.h, zd);
+    yn.fetch(yr.base(next) + next_src * yh, dxn);
+    zn.fetch(zr.base(next) + next_src * zh, zd);
     Frag pb[NJ];
+    const auto ztile = [&](int t) { return zs + 16 * ((w - t) & 3) * ZS; };
     if constexpr (!state_only) {
       if constexpr (!even) {
         if (a.dx >= EL)
@@ -403,27 +444,28 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       }
       if (src == 0) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          acc[j] = f4{0, 0, 0, 0};
+        for (int j = 0; j < 4; ++j) acc[j] = f4{0, 0, 0, 0};
 #pragma unroll
-          for (int i = 0; i < NX; ++i) acc[j] = O::mma(O::along(rs + (16 * j + m) * YS + i * KB, g), xn[i], acc[j]);
-        }
+        for (int i = 0; i < NX; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j] = O::mma(O::along(rs + (16 * j + m) * YS + i * KB, g), xn[i], acc[j]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] *= xf;
       }
       f4 P[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        P[j] = f4{0, 0, 0, 0};
-        if (j > w) continue;
+      for (int t = 0; t < 4; ++t) P[t] = f4{0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < NX; ++i) P[j] = O::mma(O::along(ys + (16 * j + m) * YS + i * KB, g), xn[i], P[j]);
+      for (int i = 0; i < NX; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) P[j][r] *= pf[j][r];
-        if (j == w)
+        for (int t = 0; t < 4; ++t)
+          P[t] = O::mma(O::along(ys + 16 * ((w - t) & 3) * YS + m * YS + i * KB, g), xn[i], P[t]);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) P[j][r] = 4 * g + r <= m ? P[j][r] : 0.0f;
-      }
+      for (int r = 0; r < 4; ++r) P[0][r] = 4 * g + r <= m ? P[0][r] * own_f[r] : 0.0f;
+#pragma unroll
+      for (int t = 1; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) P[t][r] = t <= w ? P[t][r] * far_f[r] * tile_f[t - 1] : 0.0f;
       fetch_x(next);
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -440,22 +482,21 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       if (!flagged) {
 #pragma unroll
         for (int k = 0; k < NJ; ++k)
-          if (k * KB <= 16 * w + 15)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = O::mma(O::down(zs + k * KB * ZS + 16 * j, ZS, g, m), pb[k], acc[j]);
+          for (int j = 0; j < 4; ++j) acc[j] = O::mma(O::down(ztile(k * O::TILES) + 16 * j, ztile(k * O::TILES + 1) + 16 * j, ZS, g, m), pb[k], acc[j]);
       } else {
 #pragma unroll
         for (int k = 0; k < NJ; ++k)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[j] = O::mma(only_finite<T>(O::down(zs + k * KB * ZS + 16 * j, ZS, g, m)), pb[k], acc[j]);
+          for (int j = 0; j < 4; ++j) acc[j] = O::mma(only_finite<T>(O::down(ztile(k * O::TILES) + 16 * j, ztile(k * O::TILES + 1) + 16 * j, ZS, g, m)), pb[k], acc[j]);
         // the products of z that are not finite, for the rows they reach
         constexpr int WORDS = 4 * NJ;
         int zat = 4 * g;
         asm volatile("" : "+v"(zat));  // (keeps this path's addresses out of the others' registers)
 #pragma unroll 1
         for (int at = 0; at < kChunk; ++at) {
-          // P of position at: in lanes of group (at / 4) % 4, values 4 (at / 16) + at % 4 of the operands
-          const int value = (at >> 4) * 4 + (at & 3), want = sizeof(T) == 2 ? value >> 1 : value;
+          // P of position at: in lanes of group (at / 4) % 4, values 4 t + at % 4 of the operands
+          const int t = w - (at >> 4), value = (t & 3) * 4 + (at & 3), want = sizeof(T) == 2 ? value >> 1 : value;
           uint32_t word = 0;
 #pragma unroll
           for (int e = 0; e < WORDS; ++e) word = e == want ? __builtin_bit_cast(u4, pb[e >> 2])[e & 3] : word;
@@ -468,27 +509,15 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
           }
         }
       }
-      if (last_src && row >= lead) {
-        T* o = out + (int64_t)(a.reverse ? n - 1 - start - row : start + row) * a.ot;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int d = col + 16 * j + 4 * g;
-          if (even ? d < a.dz : d + 4 <= a.dz) {
-            store_run<T, 4>(o + d, (const float*)&acc[j]);
-          } else if (!even) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (d + e < a.dz) o[d + e] = from_f32<T>(acc[j][e]);
-          }
-        }
-      }
+      if (last_src) store_rows<T, even>(acc, outp + (start + row) * out_turn, row >= lead, zd, g);
     }
     if (src == 0)
 #pragma unroll
       for (int i = 0; i < MT; ++i) R[i] *= rf;
 #pragma unroll
     for (int k = 0; k < NJ; ++k) {
-      const Frag own = O::down(zs + k * KB * ZS + 16 * w, ZS, g, m);
+      const T* zt = zs + k * KB * ZS + 16 * w;
+      const Frag own = O::down(zt, zt + 16 * ZS, ZS, g, m);
       if constexpr (sizeof(T) == 2) {
         // gamma^(..) z in bf16 parts, the next one of what the last left out
         const u4 raw = __builtin_bit_cast(u4, own);
@@ -496,8 +525,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
         u4 part[kParts];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          rest[2 * e] = __uint_as_float(raw[e] << 16) * zf[k][2 * e];
-          rest[2 * e + 1] = __uint_as_float(raw[e] & 0xffff0000u) * zf[k][2 * e + 1];
+          const float f = tile_f[3 - 2 * k - (e >> 1)];
+          rest[2 * e] = __uint_as_float(raw[e] << 16) * (pos_f[2 * e & 3] * f);
+          rest[2 * e + 1] = __uint_as_float(raw[e] & 0xffff0000u) * (pos_f[(2 * e + 1) & 3] * f);
         }
 #pragma unroll
         for (int q = 0; q < kParts; ++q)
@@ -507,18 +537,26 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
             rest[2 * e] -= __uint_as_float(part[q][e] << 16);
             rest[2 * e + 1] -= __uint_as_float(part[q][e] & 0xffff0000u);
           }
+        // four tiles of rows in turn: a product's accumulator is four products old
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          const Frag y = O::down(ys + k * KB * YS + 16 * i, YS, g, m);
+        for (int i = 0; i < MT; i += 4) {
+          Frag y[4];
 #pragma unroll
-          for (int q = 0; q < kParts; ++q) R[i] = O::mma(y, __builtin_bit_cast(Frag, part[q]), R[i]);
+          for (int e = 0; e < 4; ++e) {
+            const T* yt = ys + k * KB * YS + 16 * (i + e);
+            y[e] = O::down(yt, yt + 16 * YS, YS, g, m);
+          }
+#pragma unroll
+          for (int q = 0; q < kParts; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) R[i + e] = O::mma(y[e], __builtin_bit_cast(Frag, part[q]), R[i + e]);
         }
       } else {
         Frag f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = own[e] * zf[k][e];
+        for (int e = 0; e < 4; ++e) f[e] = own[e] * (pos_f[e] * tile_f[3 - k]);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) R[i] = O::mma(O::down(ys + k * KB * YS + 16 * i, YS, g, m), f, R[i]);
+        for (int i = 0; i < MT; ++i) R[i] = O::mma(O::down(ys + k * KB * YS + 16 * i, nullptr, YS, g, m), f, R[i]);
       }
     }
     __syncthreads();
