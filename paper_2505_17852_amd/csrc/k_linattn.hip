@@ -52,7 +52,6 @@ namespace zo {
 namespace {
 
 constexpr int kChunk = 64;    // positions
-constexpr int kSlice = 64;    // columns of z per workgroup
 constexpr int kThreads = 256;
 constexpr int kXcds = 8;
 constexpr int kParts = 3;     // bf16 parts of the decayed z in the state's sum
@@ -169,6 +168,11 @@ __device__ __forceinline__ typename Op<T>::Frag only_finite(typename Op<T>::Frag
   return __builtin_bit_cast(typename Op<T>::Frag, v);
 }
 
+// A value that all lanes share, in a scalar register.
+__device__ __forceinline__ float scalar(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(x)));
+}
+
 // gamma^n; gamma^0 is 1 whatever gamma.
 __device__ __forceinline__ float decay(float lg, int n) { return n == 0 ? 1.0f : exp2f(lg * (float)n); }
 
@@ -274,19 +278,19 @@ __device__ __forceinline__ void store_rows(const f4 (&acc)[4], T* row, bool exis
   }
 }
 
-template <typename T, int DX, bool even, bool state_only>
+template <typename T, int DX, int SL, bool even, bool state_only>
 __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 2 : 1) void linattn_chunk_kernel(LinCall c, Plan pl) {
   typedef Op<T> O;
   typedef typename O::Frag Frag;
   typedef Staged<T, DX, even> Y;
-  typedef Staged<T, kSlice, even> Z;
+  typedef Staged<T, SL, even> Z;
   constexpr int EL = 16 / sizeof(T), KB = O::KB;
   constexpr int YS = Y::STRIDE, ZS = Z::STRIDE;
   constexpr int NX = DX / KB, NJ = kChunk / KB;        // operand sets along a row of x, over the chunk's positions
-  constexpr int MT = DX / 16;                          // tiles of 16 rows of R
+  constexpr int MT = DX / 16, NW = SL / 64;           // tiles of 16: R's rows, a wave's of its columns
   __shared__ __align__(16) T ys[kChunk * YS];
   __shared__ __align__(16) T zs[kChunk * ZS];
-  __shared__ __align__(16) T rs[state_only ? 1 : kSlice * YS];  // R^T where x reads it
+  __shared__ __align__(16) T rs[state_only ? 1 : SL * YS];  // R^T where x reads it
   __shared__ int bad[2];
 
   // groups go round the XCDs (workgroup i runs on XCD i % 8), the members of one stay together
@@ -295,13 +299,13 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   if (group >= pl.groups) return;
   int member = (int)(turn % pl.members), pass = 0;
   for (;; ++pass) {
-    const int n = (state_only ? 1 : c.pass[pass].heads) * ((c.pass[pass].dz + kSlice - 1) / kSlice);
+    const int n = (state_only ? 1 : c.pass[pass].heads) * ((c.pass[pass].dz + SL - 1) / SL);
     if (member < n) break;
     member -= n;
   }
   const LinPass& a = c.pass[pass];
-  const int slices = (a.dz + kSlice - 1) / kSlice;
-  const int col = member % slices * kSlice;
+  const int slices = (a.dz + SL - 1) / SL;
+  const int col = member % slices * SL;
   const int seg = (int)(group % (pl.segments - (state_only ? 1 : 0)));
   const int64_t bh = group / (pl.segments - (state_only ? 1 : 0));
   const int b = (int)(bh / c.kv_heads), kvh = (int)(bh % c.kv_heads);
@@ -317,15 +321,15 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   if constexpr (state_only) {
     if (r0 + pl.length > n) return;  // no position follows it
   } else {
-    const int end = min(c.T, r0 + pl.length), width = min(kSlice, a.dz - col);
+    const int end = min(c.T, r0 + pl.length), width = min(SL, a.dz - col);
     for (int t = max(r0, n) + w; t < end; t += kThreads / 64)
-      if (lane < width) out[t * a.ot + col + lane] = from_f32<T>(0.0f);
+      for (int d = lane; d < width; d += 64) out[t * a.ot + col + d] = from_f32<T>(0.0f);
     if (r0 >= n && seg > 0) return;
   }
 
-  // R: rows 16 i + 4 g + r, column col + 16 w + m
-  f4 R[MT];
-  const int rz = col + 16 * w + m;
+  // R: rows 16 i + 4 g + r, columns col + 16 (w NW + u) + m
+  f4 R[NW][MT];
+  const int rz = col + 16 * w * NW + m;
   {
     const float* from = nullptr;
     bool turned = false;
@@ -336,18 +340,24 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       from = pl.states[pass] + (bh * (pl.segments - 1) + seg - 1) * a.dx * a.dz;
     }
 #pragma unroll
-    for (int i = 0; i < MT; ++i) R[i] = f4{0, 0, 0, 0};
+    for (int u = 0; u < NW; ++u)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) R[u][i] = f4{0, 0, 0, 0};
     if (from) {
       const int sx = turned ? 1 : a.dz, sz = turned ? a.dx : 1;
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+      for (int u = 0; u < NW; ++u) {
+        const int z = rz + 16 * u;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) R[i][r] = from[min(16 * i + 4 * g + r, a.dx - 1) * sx + min(rz, a.dz - 1) * sz];
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+          for (int r = 0; r < 4; ++r) R[u][i][r] = from[min(16 * i + 4 * g + r, a.dx - 1) * sx + min(z, a.dz - 1) * sz];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (16 * i + 4 * g + r >= a.dx || rz >= a.dz) R[i][r] = 0.0f;
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (16 * i + 4 * g + r >= a.dx || z >= a.dz) R[u][i][r] = 0.0f;
+      }
     }
   }
 
@@ -366,15 +376,18 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
     far_f[r] = state_only ? 0.0f : a.score * decay(lg, apart + 16);
     pos_f[r] = a.upd * decay(lg, 16 - off - 4 * g - r);
   }
-  const float tile_f[4] = {1.0f, decay(lg, 16), decay(lg, 32), decay(lg, 48)};
+  const float tile_f[4] = {1.0f, scalar(decay(lg, 16)), scalar(decay(lg, 32)), scalar(decay(lg, 48))};
   // of the carried state: what reaches a row, and what is left after the chunk
-  float xf = a.carry * decay(lg, max(row - lead0, 0) + off), rf = decay(lg, kChunk - lead0);
+  float xf = a.carry * decay(lg, max(row - lead0, 0) + off), rf = scalar(decay(lg, kChunk - lead0));
 
   // the next step's y and z, the next chunk's x (whose values past dx meet zeros of y and R)
-  const int origin = a.reverse ? n - 1 : 0, zd = min(kSlice, a.dz - col);
+  const int origin = a.reverse ? n - 1 : 0, zd = min(SL, a.dz - col);
   const Rows<T> yr((const T*)a.y.p + b * a.y.b + (int64_t)kvh * a.sources * a.y.h, a.y.t, a.reverse, origin);
   const Rows<T> zr((const T*)a.z.p + b * a.z.b + (int64_t)kvh * a.sources * a.z.h + col, a.z.t, a.reverse, origin);
   const Rows<T> xr((const T*)a.x.p + b * a.x.b + (int64_t)h * a.x.h, a.x.t, a.reverse, origin);
+  // The loads of the next step go out once this one's tiles are in LDS, or, where the registers of two waves
+  // per SIMD do not hold them beside the output, once that is stored.
+  constexpr bool late = sizeof(T) == 2 && SL == 128;
   // (kept in scalar registers: loads of arguments inside the loop would wait for the LDS too)
   int64_t yh = a.y.h, zh = a.z.h, out_turn = a.reverse ? -a.ot : a.ot;
   T* outp = out + origin * a.ot + col;
@@ -409,9 +422,10 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   }
   if (tid < 2) bad[tid] = 0;
   if (a.dx < DX) Y::clear(ys);
-  if (zd < kSlice) Z::clear(zs);
+  if (zd < SL) Z::clear(zs);
   __syncthreads();
-  f4 acc[4];
+  static_assert(SL == 64 || SL == 128, "");
+  f4 acc[4];  // (with two parts of the output every step is a chunk of its own: one source)
   int src = 0, turn_of = 0;
   for (int start = r0 - lead0; start < r1; turn_of ^= 1) {
     const int lead = max(r0 - start, 0);
@@ -421,7 +435,10 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       if (zn.any_not_finite()) bad[turn_of] = 1;
       if (src == 0)
 #pragma unroll
-        for (int i = 0; i < MT; ++i) store_run<T, 4>(rs + (16 * w + m) * YS + 16 * i + 4 * g, (const float*)&R[i]);
+        for (int u = 0; u < NW; ++u)
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+            store_run<T, 4>(rs + (16 * (w * NW + u) + m) * YS + 16 * i + 4 * g, (const float*)&R[u][i]);
     }
     __syncthreads();
     const bool flagged = !state_only && bad[turn_of];
@@ -429,11 +446,15 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
     // the loads of the next step, or once more this one's after the last
     const bool last_src = src == sources - 1;
     const int next = last_src && start + kChunk < r1 ? start + kChunk : start, next_src = last_src ? 0 : src + 1;
-    if (next > start && lead) aim(0);
-    yn.fetch(yr.base(next) + next_src * yh, dxn);
-    zn.fetch(zr.base(next) + next_src * zh, zd);
-    Frag pb[NJ];
-    const auto ztile = [&](int t) { return zs + 16 * ((w - t) & 3) * ZS; };
+    if (next > start && lead) {
+      int none = 0;
+      asm volatile("" : "+v"(none));  // (worked out here, not held in registers from before the loop)
+      aim(none);
+    }
+    if constexpr (!late) {
+      yn.fetch(yr.base(next) + next_src * yh, dxn);
+      zn.fetch(zr.base(next) + next_src * zh, zd);
+    }
     if constexpr (!state_only) {
       if constexpr (!even) {
         if (a.dx >= EL)
@@ -441,16 +462,6 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
           for (int i = 0; i < NX; ++i)
             if ((i + 1) * KB > a.dx - EL)
               xn[i] = __builtin_bit_cast(Frag, drop<T>(__builtin_bit_cast(u4, xn[i]), min(max(i * KB + KB / 4 * g - (a.dx - EL), 0), EL - 1)));
-      }
-      if (src == 0) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = f4{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < NX; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[j] = O::mma(O::along(rs + (16 * j + m) * YS + i * KB, g), xn[i], acc[j]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] *= xf;
       }
       f4 P[4];
 #pragma unroll
@@ -466,105 +477,138 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       for (int t = 1; t < 4; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) P[t][r] = t <= w ? P[t][r] * far_f[r] * tile_f[t - 1] : 0.0f;
-      fetch_x(next);
-      if constexpr (sizeof(T) == 2) {
+      Frag pb[NJ];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+      for (int j = 0; j < NJ; ++j) {
+        if constexpr (sizeof(T) == 2)
           pb[j] = __builtin_bit_cast(Frag, u4{bf16_pair(P[2 * j][0], P[2 * j][1]), bf16_pair(P[2 * j][2], P[2 * j][3]),
                                               bf16_pair(P[2 * j + 1][0], P[2 * j + 1][1]),
                                               bf16_pair(P[2 * j + 1][2], P[2 * j + 1][3])});
-      } else {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) pb[j] = P[j];
+        else
+          pb[j] = P[j];
       }
-    }
-    if constexpr (!state_only) {
-      if (!flagged) {
+      // the output, 64 columns at a time
 #pragma unroll
-        for (int k = 0; k < NJ; ++k)
+      for (int part = 0; part < SL / 64; ++part) {
+        if (src == 0) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[j] = O::mma(O::down(ztile(k * O::TILES) + 16 * j, ztile(k * O::TILES + 1) + 16 * j, ZS, g, m), pb[k], acc[j]);
-      } else {
+          for (int j = 0; j < 4; ++j) acc[j] = f4{0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < NJ; ++k)
+          for (int i = 0; i < NX; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[j] = O::mma(only_finite<T>(O::down(ztile(k * O::TILES) + 16 * j, ztile(k * O::TILES + 1) + 16 * j, ZS, g, m)), pb[k], acc[j]);
-        // the products of z that are not finite, for the rows they reach
-        constexpr int WORDS = 4 * NJ;
-        int zat = 4 * g;
-        asm volatile("" : "+v"(zat));  // (keeps this path's addresses out of the others' registers)
+            for (int j = 0; j < 4; ++j)
+              acc[j] = O::mma(O::along(rs + (64 * part + 16 * j + m) * YS + i * KB, g), xn[i], acc[j]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j] *= xf;
+        }
+        // tile t of the scores meets the rows of z of its positions
+        const auto z_of = [&](int k, int j) {
+          const auto tile = [&](int t) { return zs + 16 * ((w - t) & 3) * ZS + 64 * part + 16 * j; };
+          return O::down(tile(k * O::TILES), tile(k * O::TILES + 1), ZS, g, m);
+        };
+        if (!flagged) {
+#pragma unroll
+          for (int k = 0; k < NJ; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = O::mma(z_of(k, j), pb[k], acc[j]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < NJ; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = O::mma(only_finite<T>(z_of(k, j)), pb[k], acc[j]);
+          // the products of z that are not finite, for the rows they reach
+          constexpr int WORDS = 4 * NJ;
+          int zat = 64 * part + 4 * g;
+          asm volatile("" : "+v"(zat));  // (keeps this path's addresses out of the others' registers)
 #pragma unroll 1
-        for (int at = 0; at < kChunk; ++at) {
-          // P of position at: in lanes of group (at / 4) % 4, values 4 t + at % 4 of the operands
-          const int t = w - (at >> 4), value = (t & 3) * 4 + (at & 3), want = sizeof(T) == 2 ? value >> 1 : value;
-          uint32_t word = 0;
+          for (int at = 0; at < kChunk; ++at) {
+            // P of position at: in lanes of group (at / 4) % 4, values 4 t + at % 4 of the operands
+            const int t = w - (at >> 4), value = (t & 3) * 4 + (at & 3), want = sizeof(T) == 2 ? value >> 1 : value;
+            uint32_t word = 0;
 #pragma unroll
-          for (int e = 0; e < WORDS; ++e) word = e == want ? __builtin_bit_cast(u4, pb[e >> 2])[e & 3] : word;
-          word = (uint32_t)__shfl((int)word, m + 16 * ((at >> 2) & 3), 64);
-          const float p = __uint_as_float(sizeof(T) == 4 ? word : at & 1 ? word & 0xffff0000u : word << 16);
+            for (int e = 0; e < WORDS; ++e) word = e == want ? __builtin_bit_cast(u4, pb[e >> 2])[e & 3] : word;
+            word = (uint32_t)__shfl((int)word, m + 16 * ((at >> 2) & 3), 64);
+            const float p = __uint_as_float(sizeof(T) == 4 ? word : at & 1 ? word & 0xffff0000u : word << 16);
 #pragma unroll
-          for (int d = 0; d < 16; ++d) {
-            const float v = to_f32(zs[at * ZS + zat + 16 * (d >> 2) + (d & 3)]);
-            if (at <= row && !(fabsf(v) < __builtin_inff())) acc[d >> 2][d & 3] += p * v;
+            for (int d = 0; d < 16; ++d) {
+              const float v = to_f32(zs[at * ZS + zat + 16 * (d >> 2) + (d & 3)]);
+              if (at <= row && !(fabsf(v) < __builtin_inff())) acc[d >> 2][d & 3] += p * v;
+            }
           }
         }
+        if (last_src)
+          store_rows<T, even>(acc, outp + (start + row) * out_turn + 64 * part, row >= lead, zd - 64 * part, g);
       }
-      if (last_src) store_rows<T, even>(acc, outp + (start + row) * out_turn, row >= lead, zd, g);
+      fetch_x(next);
+    }
+    if constexpr (late) {
+      yn.fetch(yr.base(next) + next_src * yh, dxn);
+      zn.fetch(zr.base(next) + next_src * zh, zd);
     }
     if (src == 0)
 #pragma unroll
-      for (int i = 0; i < MT; ++i) R[i] *= rf;
+      for (int u = 0; u < NW; ++u)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) R[u][i] *= rf;
 #pragma unroll
     for (int k = 0; k < NJ; ++k) {
-      const T* zt = zs + k * KB * ZS + 16 * w;
-      const Frag own = O::down(zt, zt + 16 * ZS, ZS, g, m);
-      if constexpr (sizeof(T) == 2) {
-        // gamma^(..) z in bf16 parts, the next one of what the last left out
-        const u4 raw = __builtin_bit_cast(u4, own);
-        float rest[8];
-        u4 part[kParts];
+      // gamma^(..) z; in bf16 parts, the next one of what the last left out
+      constexpr int PARTS = sizeof(T) == 2 ? kParts : 1;
+      Frag part[NW][PARTS];
+#pragma unroll
+      for (int u = 0; u < NW; ++u) {
+        const T* zt = zs + k * KB * ZS + 16 * (w * NW + u);
+        const Frag own = O::down(zt, zt + 16 * ZS, ZS, g, m);
+        if constexpr (sizeof(T) == 2) {
+          const u4 raw = __builtin_bit_cast(u4, own);
+          float rest[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float f = tile_f[3 - 2 * k - (e >> 1)];
+            rest[2 * e] = __uint_as_float(raw[e] << 16) * (pos_f[2 * e & 3] * f);
+            rest[2 * e + 1] = __uint_as_float(raw[e] & 0xffff0000u) * (pos_f[(2 * e + 1) & 3] * f);
+          }
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q) {
+            u4 p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              p[e] = bf16_pair(rest[2 * e], rest[2 * e + 1]);
+              rest[2 * e] -= __uint_as_float(p[e] << 16);
+              rest[2 * e + 1] -= __uint_as_float(p[e] & 0xffff0000u);
+            }
+            part[u][q] = __builtin_bit_cast(Frag, p);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) part[u][0][e] = own[e] * (pos_f[e] * tile_f[3 - k]);
+        }
+      }
+      // four tiles of rows in turn: a product's accumulator is four products old
+#pragma unroll
+      for (int i = 0; i < MT; i += 4) {
+        Frag y[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float f = tile_f[3 - 2 * k - (e >> 1)];
-          rest[2 * e] = __uint_as_float(raw[e] << 16) * (pos_f[2 * e & 3] * f);
-          rest[2 * e + 1] = __uint_as_float(raw[e] & 0xffff0000u) * (pos_f[(2 * e + 1) & 3] * f);
+          const T* yt = ys + k * KB * YS + 16 * (i + e);
+          y[e] = O::down(yt, yt + 16 * YS, YS, g, m);
         }
 #pragma unroll
-        for (int q = 0; q < kParts; ++q)
+        for (int q = 0; q < PARTS; ++q)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            part[q][e] = bf16_pair(rest[2 * e], rest[2 * e + 1]);
-            rest[2 * e] -= __uint_as_float(part[q][e] << 16);
-            rest[2 * e + 1] -= __uint_as_float(part[q][e] & 0xffff0000u);
-          }
-        // four tiles of rows in turn: a product's accumulator is four products old
+          for (int u = 0; u < NW; ++u)
 #pragma unroll
-        for (int i = 0; i < MT; i += 4) {
-          Frag y[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const T* yt = ys + k * KB * YS + 16 * (i + e);
-            y[e] = O::down(yt, yt + 16 * YS, YS, g, m);
-          }
-#pragma unroll
-          for (int q = 0; q < kParts; ++q)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) R[i + e] = O::mma(y[e], __builtin_bit_cast(Frag, part[q]), R[i + e]);
-        }
-      } else {
-        Frag f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = own[e] * (pos_f[e] * tile_f[3 - k]);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) R[i] = O::mma(O::down(ys + k * KB * YS + 16 * i, nullptr, YS, g, m), f, R[i]);
+            for (int e = 0; e < 4; ++e) R[u][i + e] = O::mma(y[e], part[u][q], R[u][i + e]);
       }
     }
     __syncthreads();
     src = next_src;
     if (last_src) {
       if (lead) {
-        xf = a.carry * decay(lg, row + off);
-        rf = decay(lg, kChunk);
+        float l = lg;
+        asm volatile("" : "+v"(l));
+        xf = a.carry * decay(l, row + off);
+        rf = scalar(decay(l, kChunk));
       }
       start += kChunk;
     }
@@ -578,14 +622,16 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
     to = a.fin + bh * a.dx * a.dz;
     turned = a.state_t;
   }
-  if (to && rz < a.dz)
+  if (to)
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int u = 0; u < NW; ++u)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int x = 16 * i + 4 * g + r;
-        if (x < a.dx) to[turned ? rz * a.dx + x : x * a.dz + rz] = R[i][r];
-      }
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int x = 16 * i + 4 * g + r, z = rz + 16 * u;
+          if (x < a.dx && z < a.dz) to[turned ? z * a.dx + x : x * a.dz + z] = R[u][i][r];
+        }
 }
 
 // Adds up the segments' states: state_s = gamma^length state_(s-1) + its own sum.
@@ -622,9 +668,7 @@ void split(int64_t workgroups, int T, int* segments, int* length) {
   *segments = T > 0 ? (T + *length - 1) / *length : 1;
 }
 
-int slices_of(int dz) { return (dz + kSlice - 1) / kSlice; }
-
-template <typename T, int DX, bool even>
+template <typename T, int DX, int SL, bool even>
 hipError_t launch_chunks(const LinCall& c, Plan pl, hipStream_t st) {
   const int64_t states = (int64_t)c.B * c.kv_heads;
   const auto grid = [&](int64_t groups, int members) {
@@ -633,14 +677,14 @@ hipError_t launch_chunks(const LinCall& c, Plan pl, hipStream_t st) {
   int slices = 0, members = 0, most = 0;
   for (int i = 0; i < c.npasses; ++i) {
     const LinPass& p = c.pass[i];
-    slices += slices_of(p.dz);
-    members += p.heads * slices_of(p.dz);
+    slices += (p.dz + SL - 1) / SL;
+    members += p.heads * ((p.dz + SL - 1) / SL);
     most = std::max(most, p.dx * p.dz);
   }
   if (pl.segments > 1) {
     pl.groups = states * (pl.segments - 1);
     pl.members = slices;
-    linattn_chunk_kernel<T, DX, even, true><<<grid(pl.groups, slices), kThreads, 0, st>>>(c, pl);
+    linattn_chunk_kernel<T, DX, SL, even, true><<<grid(pl.groups, slices), kThreads, 0, st>>>(c, pl);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (pl.segments > 2) {
@@ -653,20 +697,29 @@ hipError_t launch_chunks(const LinCall& c, Plan pl, hipStream_t st) {
   }
   pl.groups = states * pl.segments;
   pl.members = members;
-  linattn_chunk_kernel<T, DX, even, false><<<grid(pl.groups, members), kThreads, 0, st>>>(c, pl);
+  linattn_chunk_kernel<T, DX, SL, even, false><<<grid(pl.groups, members), kThreads, 0, st>>>(c, pl);
   return hipGetLastError();
 }
 
 template <typename T, bool even>
-hipError_t launch(const LinCall& c, const Plan& pl, int dx, hipStream_t st) {
-  if (dx <= 64) return launch_chunks<T, 64, even>(c, pl, st);
-  if (dx <= 128) return launch_chunks<T, 128, even>(c, pl, st);
-  return launch_chunks<T, 256, even>(c, pl, st);
+hipError_t launch(const LinCall& c, const Plan& pl, int dx, int slice, hipStream_t st) {
+  if (dx <= 64) return launch_chunks<T, 64, 64, even>(c, pl, st);
+  if (dx > 128) return launch_chunks<T, 256, 64, even>(c, pl, st);
+  return slice == 128 ? launch_chunks<T, 128, 128, even>(c, pl, st) : launch_chunks<T, 128, 64, even>(c, pl, st);
+}
+
+// Columns of z per workgroup: 128 where states have more than 64 rows and columns and no more
+// than 128 rows (x and y are then read once, and the scores formed once), 64 otherwise, and where
+// several query heads add to one output.
+int slice_of(int dk, int dv, int share, bool backward) {
+  if (backward && share > 1) return 64;
+  const int dx = backward ? std::max(dk, dv) : dk, dz = backward ? std::min(dk, dv) : dv;
+  return dx > 64 && dx <= 128 && dz > 64 ? 128 : 64;
 }
 
 void plan_segments(int B, int kv_heads, int share, int dk, int dv, int T, bool backward, Plan* pl) {
-  const int64_t per_state = backward ? (int64_t)share * slices_of(dk) + slices_of(dk) + slices_of(dv)
-                                     : (int64_t)share * slices_of(dv);
+  const int sl = slice_of(dk, dv, share, backward), nk = (dk + sl - 1) / sl, nv = (dv + sl - 1) / sl;
+  const int64_t per_state = backward ? (int64_t)share * nk + nk + nv : (int64_t)share * nv;
   split((int64_t)B * kv_heads * per_state, T, &pl->segments, &pl->length);
 }
 
@@ -684,7 +737,8 @@ hipError_t launch_linattn(const LinCall& c, hipStream_t s) {
   const LinPass& p = c.pass[0];
   const bool backward = c.npasses > 1;
   Plan pl{};
-  plan_segments(c.B, c.kv_heads, c.share, backward ? p.dz : p.dx, backward ? p.dx : p.dz, c.T, backward, &pl);
+  const int dk = backward ? p.dz : p.dx, dv = backward ? p.dx : p.dz, sl = slice_of(dk, dv, c.share, backward);
+  plan_segments(c.B, c.kv_heads, c.share, dk, dv, c.T, backward, &pl);
   bool even = true;
   int dx = 0;
   for (int i = 0; i < c.npasses; ++i) {
@@ -693,8 +747,9 @@ hipError_t launch_linattn(const LinCall& c, hipStream_t s) {
     const int el = c.dtype == ZO_WBF16 ? 8 : 4;
     even &= c.pass[i].dx % el == 0 && c.pass[i].dz % el == 0;
   }
-  if (c.dtype == ZO_WBF16) return even ? launch<uint16_t, true>(c, pl, dx, s) : launch<uint16_t, false>(c, pl, dx, s);
-  return even ? launch<float, true>(c, pl, dx, s) : launch<float, false>(c, pl, dx, s);
+  if (c.dtype == ZO_WBF16)
+    return even ? launch<uint16_t, true>(c, pl, dx, sl, s) : launch<uint16_t, false>(c, pl, dx, sl, s);
+  return even ? launch<float, true>(c, pl, dx, sl, s) : launch<float, false>(c, pl, dx, sl, s);
 }
 
 }  // namespace zo
