@@ -11,9 +11,12 @@
 // by lane exchanges; codes are the nearest in the square root of the first
 // moment and the fourth root of the second (relative steps of 1.6% at the
 // block's maximum, and a range of 1.6e4 and 4e9 below it). The code of a value
-// near a rounding boundary depends on the last bit of the moment, so the
-// operations are those of the definition, one IEEE rounding each, without
-// contraction.
+// near a rounding boundary depends on the last bit of the moment, so moments and
+// codes are those of the definition's operations, one IEEE rounding each, without
+// contraction. Roots and quotients of that kind take ten instructions and
+// more; a code is first found from the hardware's approximate ones (a few units in the last
+// place off) and worked out again only where it lies within 2^-11 of a boundary,
+// which their error cannot reach across.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -91,16 +94,29 @@ __device__ __forceinline__ float decode_v(int c, float top) {
   part = part * part;
   return part * part * top;
 }
-__device__ __forceinline__ int encode_m(float m, float top) {
+constexpr float kNear = 0x1p-11f;
+
+// Whether the nearest whole number of t, at most 255 and known to 2^-18 relative, is certain (not of a NaN).
+__device__ __forceinline__ bool certain(float t) { return fabsf(t - rintf(t)) < 0.5f - kNear; }
+
+__device__ __noinline__ float exact_code(float x, float top, int root) {
 #pragma clang fp contract(off)
-  const float share = fabsf(m) / top;
-  const float code = rintf(sqrtf(share >= 0.0f ? share : 0.0f) * 127.0f);
+  const float share = x / top;
+  float r = sqrtf(share >= 0.0f ? share : 0.0f);
+  if (root == 4) r = sqrtf(r);
+  return rintf(r * (root == 4 ? 255.0f : 127.0f));
+}
+// inv: 1 / top.
+__device__ __forceinline__ int encode_m(float m, float top, float inv) {
+  const float t = __builtin_amdgcn_sqrtf(fabsf(m) * inv) * 127.0f;
+  float code = rintf(t);
+  if (!certain(t)) code = exact_code(fabsf(m), top, 2);
   return m < 0.0f ? -(int)code : (int)code;
 }
-__device__ __forceinline__ int encode_v(float v, float top) {
-#pragma clang fp contract(off)
-  const float share = v / top;
-  const float code = rintf(sqrtf(sqrtf(share >= 0.0f ? share : 0.0f)) * 255.0f);
+__device__ __forceinline__ int encode_v(float v, float top, float inv) {
+  const float t = __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(v * inv)) * 255.0f;
+  float code = rintf(t);
+  if (!certain(t)) code = exact_code(v, top, 4);
   return v > 0.0f ? max((int)code, 1) : 0;
 }
 
@@ -150,7 +166,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Args a) {
     const float ge = a.grad_scale ? g[e] * gs : g[e];
     m[e] = m[e] * a.b1 + ge * a.omb1;
     v[e] = v[e] * a.b2 + (ge * ge) * a.omb2;
-    const float change = (m[e] * a.c1) / (sqrtf(v[e] * a.c2) + a.eps);
+    // (the quotient is scaled by lr, far below the parameter: the approximate root and reciprocal serve)
+    const float change = (m[e] * a.c1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e] * a.c2) + a.eps);
     p[e] = p[e] * t.keep - change * a.lr;
   }
   if (t.pbf) store8((uint16_t*)t.p + j, left, p);
@@ -163,13 +180,14 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Args a) {
     }
     mtop = block_top(m);
     vtop = block_top(v);
+    const float minv = 1.0f / mtop, vinv = 1.0f / vtop;
     uint2 mc{0, 0}, vc{0, 0};
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
       uint32_t& mw = e < 4 ? mc.x : mc.y;
       uint32_t& vw = e < 4 ? vc.x : vc.y;
-      mw |= (uint32_t)(uint8_t)encode_m(m[e], mtop) << (8 * (e & 3));
-      vw |= (uint32_t)(uint8_t)encode_v(v[e], vtop) << (8 * (e & 3));
+      mw |= (uint32_t)(uint8_t)encode_m(m[e], mtop, minv) << (8 * (e & 3));
+      vw |= (uint32_t)(uint8_t)encode_v(v[e], vtop, vinv) << (8 * (e & 3));
     }
     *(uint2*)((int8_t*)a.m + s) = mc;
     *(uint2*)((uint8_t*)a.v + s) = vc;

@@ -63,20 +63,44 @@ constexpr int vals_of() { return TPR > 256 ? 8 : 16; }
 template <typename T>
 constexpr int vec_of() { return sizeof(T) == 2 ? 8 : 4; }
 
-template <typename T, int TPR, int VEC>
-__device__ __forceinline__ void load_row(const T* p, int lane, int D, float* out, float fill) {
-  constexpr int kVals = vals_of<TPR>();
+// A row as it lies in memory, on its way to a thread's registers. even: D is a multiple of VEC, and runs past
+// the end repeat the last one (no branch around a load: the next row's loads stay in flight while
+// this one is worked on).
+template <typename T, int TPR, bool even, int VEC = vec_of<T>()>
+struct RawRow {
+  static constexpr int N = vals_of<TPR>() / VEC;
+  Run<T, VEC> v[N];
+  __device__ __forceinline__ void load(const T* p, int lane, int D) {
 #pragma unroll
-  for (int c = 0; c < kVals / VEC; ++c) {
-    const int j = (c * TPR + lane) * VEC;
-    if (j + VEC <= D) {
-      load_run<T, VEC>(p + j, out + c * VEC);
-    } else {
+    for (int c = 0; c < N; ++c) {
+      const int j = (c * TPR + lane) * VEC;
+      if constexpr (even) {
+        v[c] = *(const Run<T, VEC>*)(p + min(j, D - VEC));
+      } else if (j + VEC <= D) {
+        v[c] = *(const Run<T, VEC>*)(p + j);
+      } else {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) out[c * VEC + e] = j + e < D ? to_f32(p[j + e]) : fill;
+        for (int e = 0; e < VEC; ++e) v[c].v[e] = p[min(j + e, D - 1)];
+      }
     }
   }
+  // fp32, zeros past the row's end
+  __device__ __forceinline__ void get(int lane, int D, float* out) const {
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      const int j = (c * TPR + lane) * VEC;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) out[c * VEC + e] = (even ? j : j + e) < D ? to_f32(v[c].v[e]) : 0.0f;
+    }
+  }
+};
+template <typename T, int TPR, bool even, int VEC>
+__device__ __forceinline__ void load_row(const T* p, int lane, int D, float* out) {
+  RawRow<T, TPR, even, VEC> r;
+  r.load(p, lane, D);
+  r.get(lane, D, out);
 }
+
 template <typename T, int TPR, int VEC>
 __device__ __forceinline__ void store_row(T* p, int lane, int D, const float* in) {
   constexpr int kVals = vals_of<TPR>();
@@ -99,26 +123,27 @@ constexpr int threads_of() { return TPR > 256 ? TPR : 256; }
 template <int TPR>
 constexpr int rows_of() { return threads_of<TPR>() / TPR; }
 
-template <typename T, typename W, int TPR>
+template <typename T, typename W, int TPR, bool even>
 __global__ __launch_bounds__(threads_of<TPR>()) void norm_kernel(NormArgs a) {
   constexpr int VEC = vec_of<T>(), RPB = rows_of<TPR>(), kVals = vals_of<TPR>();
   __shared__ float buf[2][TPR / 64][1];
   const int lane = threadIdx.x % TPR, D = (int)a.D;
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+  RawRow<T, TPR, even> raw;
+  if (r < a.rows) raw.load((const T*)a.x + r * a.xs, lane, D);
   float w[kVals], b[kVals];
-  bool loaded = false;
-  for (int64_t r = block_id() * RPB + threadIdx.x / TPR; r < a.rows; r += (int64_t)gridDim.x * gridDim.y * RPB) {
-    float x[kVals];
-    load_row<T, TPR, VEC>((const T*)a.x + r * a.xs, lane, D, x, 0.0f);
-    if (!loaded) {
-      loaded = true;
 #pragma unroll
-      for (int i = 0; i < kVals; ++i) {
-        w[i] = 1.0f;
-        b[i] = 0.0f;
-      }
-      if (a.w) load_row<W, TPR, VEC>((const W*)a.w, lane, D, w, 0.0f);
-      if (a.b) load_row<W, TPR, VEC>((const W*)a.b, lane, D, b, 0.0f);
-    }
+  for (int i = 0; i < kVals; ++i) {
+    w[i] = 1.0f;
+    b[i] = 0.0f;
+  }
+  if (a.w) load_row<W, TPR, even, VEC>((const W*)a.w, lane, D, w);
+  if (a.b) load_row<W, TPR, even, VEC>((const W*)a.b, lane, D, b);
+  for (; r < a.rows; r += step) {
+    float x[kVals];
+    raw.get(lane, D, x);
+    raw.load((const T*)a.x + (r + step < a.rows ? r + step : r) * a.xs, lane, D);
     float s[1] = {0};
 #pragma unroll
     for (int i = 0; i < kVals; ++i) s[0] += x[i];
@@ -130,7 +155,8 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_kernel(NormArgs a) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         float& v = x[c * VEC + e];
-        v = (c * TPR + lane) * VEC + e < D ? v - mean : 0.0f;
+        const int j = (c * TPR + lane) * VEC;
+        v = (even ? j : j + e) < D ? v - mean : 0.0f;
         s[0] += v * v;
       }
     row_sums<TPR, 1>(s, buf[1]);
@@ -145,12 +171,23 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_kernel(NormArgs a) {
   }
 }
 
-template <typename T, typename W, int TPR>
+template <typename T, typename W, int TPR, bool even>
 __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormArgs a) {
   constexpr int VEC = vec_of<T>(), RPB = rows_of<TPR>(), NT = threads_of<TPR>(), kVals = vals_of<TPR>();
   __shared__ float buf[2][TPR / 64][2];
   __shared__ float join[RPB > 1 ? kVals * NT : 1];
   const int lane = threadIdx.x % TPR, D = (int)a.D;
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+  RawRow<T, TPR, even> rx, rdy;
+  float mean = 0, rstd = 0;
+  const auto load = [&](int64_t r) {
+    rx.load((const T*)a.x + r * a.xs, lane, D);
+    rdy.load((const T*)a.dy + r * a.dys, lane, D);
+    mean = a.mean[r];
+    rstd = a.rstd[r];
+  };
+  if (r < a.rows) load(r);
   float w[kVals], dw[kVals], db[kVals];
 #pragma unroll
   for (int i = 0; i < kVals; ++i) {
@@ -158,17 +195,20 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormAr
     dw[i] = 0.0f;
     db[i] = 0.0f;
   }
-  if (a.w) load_row<W, TPR, VEC>((const W*)a.w, lane, D, w, 0.0f);
+  if (a.w) load_row<W, TPR, even, VEC>((const W*)a.w, lane, D, w);
   int turn = 0;
-  for (int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; r < a.rows; r += (int64_t)gridDim.x * RPB) {
+  for (; r < a.rows; r += step) {
     float x[kVals], dy[kVals];
-    load_row<T, TPR, VEC>((const T*)a.x + r * a.xs, lane, D, x, 0.0f);
-    load_row<T, TPR, VEC>((const T*)a.dy + r * a.dys, lane, D, dy, 0.0f);
-    const float mean = a.mean[r], rstd = a.rstd[r];
+    rx.get(lane, D, x);
+    rdy.get(lane, D, dy);
+    const float rs = rstd;
+#pragma unroll
+    for (int i = 0; i < kVals; ++i) x[i] = (x[i] - mean) * rs;  // past the row's end dy is zero, and x never stored
+    // the next row's loads before this one's sums (the last row has none: itself once more, in place or not)
+    load(r + step < a.rows ? r + step : r);
     float s[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < kVals; ++i) {
-      x[i] = (x[i] - mean) * rstd;  // past the row's end dy is zero, and x never stored
       db[i] += dy[i];
       dw[i] += dy[i] * x[i];
       dy[i] *= w[i];
@@ -179,7 +219,7 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormAr
     turn ^= 1;
     const float m0 = s[0] / (float)D, m1 = s[1] / (float)D;
 #pragma unroll
-    for (int i = 0; i < kVals; ++i) x[i] = rstd * (dy[i] - m0 - x[i] * m1);
+    for (int i = 0; i < kVals; ++i) x[i] = rs * (dy[i] - m0 - x[i] * m1);
     store_row<T, TPR, VEC>((T*)a.y + r * a.ys, lane, D, x);
   }
   if (!a.partial) return;
@@ -207,23 +247,29 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormAr
   store_row<float, TPR, VEC>(part + D, lane, D, db);
 }
 
-// Adds the workgroups' sums: 64 columns by 4 shares of the workgroups, then the shares.
-__global__ __launch_bounds__(256) void norm_sums_kernel(const float* partial, int parts, int64_t D, float* dw,
-                                                        float* db) {
-  __shared__ float join[4][64];
+// Adds the workgroups' sums: 64 columns by 16 shares of the workgroups, then the shares (a tree, so that no chain of
+// loads is longer than 32).
+__global__ __launch_bounds__(1024) void norm_sums_kernel(const float* partial, int parts, int64_t D, float* dw,
+                                                         float* db) {
+  __shared__ float join[16][64];
   float* out = blockIdx.y ? db : dw;
   if (!out) return;
-  const int64_t j = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-  const int share = threadIdx.x >> 6;
+  const int c = threadIdx.x & 63, share = threadIdx.x >> 6;
+  const int64_t j = (int64_t)blockIdx.x * 64 + c;
   float s = 0;
   if (j < D) {
     const float* p = partial + blockIdx.y * D + j;
 #pragma unroll 8
-    for (int k = share; k < parts; k += 4) s += p[(int64_t)k * 2 * D];
+    for (int k = share; k < parts; k += 16) s += p[(int64_t)k * 2 * D];
   }
-  join[share][threadIdx.x & 63] = s;
+  join[share][c] = s;
   __syncthreads();
-  if (share == 0 && j < D) out[j] = (join[0][threadIdx.x] + join[1][threadIdx.x]) + (join[2][threadIdx.x] + join[3][threadIdx.x]);
+#pragma unroll
+  for (int half = 8; half; half >>= 1) {
+    if (share < half) join[share][c] += join[share + half][c];
+    __syncthreads();
+  }
+  if (share == 0 && j < D) out[j] = join[0][c];
 }
 
 // Rows of any length: a workgroup per row, every pass reads the row again.
@@ -303,34 +349,47 @@ int parts_of(int64_t rows, int64_t D) {
   return (int)(need < kMaxParts ? need : kMaxParts);
 }
 
-template <typename T, typename W>
-hipError_t forward(const NormArgs& a, hipStream_t s) {
+// Workgroups of a forward pass: each keeps weight and bias for all its rows.
+constexpr int kMaxForward = 2048;
+
+template <typename T, typename W, bool even>
+hipError_t forward_as(const NormArgs& a, hipStream_t s) {
   const int tpr = row_threads(a.D);
-  const dim3 grid = wide_grid(tpr == 64 ? (a.rows + 3) / 4 : a.rows);
-  if (tpr == 64) norm_kernel<T, W, 64><<<grid, 256, 0, s>>>(a);
-  else if (tpr == 256) norm_kernel<T, W, 256><<<grid, 256, 0, s>>>(a);
-  else if (tpr == 1024) norm_kernel<T, W, 1024><<<grid, 1024, 0, s>>>(a);
-  else norm_loop_kernel<T, W><<<grid, kLoopThreads, 0, s>>>(a);
+  const int64_t need = tpr == 64 ? (a.rows + 3) / 4 : a.rows;
+  const unsigned grid = (unsigned)(need < kMaxForward ? need : kMaxForward);
+  if (tpr == 64) norm_kernel<T, W, 64, even><<<grid, 256, 0, s>>>(a);
+  else if (tpr == 256) norm_kernel<T, W, 256, even><<<grid, 256, 0, s>>>(a);
+  else if (tpr == 1024) norm_kernel<T, W, 1024, even><<<grid, 1024, 0, s>>>(a);
+  else norm_loop_kernel<T, W><<<wide_grid(a.rows), kLoopThreads, 0, s>>>(a);
   return hipGetLastError();
 }
+template <typename T, typename W>
+hipError_t forward(const NormArgs& a, hipStream_t s) {
+  return a.D % vec_of<T>() == 0 ? forward_as<T, W, true>(a, s) : forward_as<T, W, false>(a, s);
+}
 
+template <typename T, typename W, bool even>
+void backward_as(const NormArgs& a, int parts, hipStream_t s) {
+  const int tpr = row_threads(a.D);
+  if (tpr == 64) norm_backward_kernel<T, W, 64, even><<<parts, 256, 0, s>>>(a);
+  else if (tpr == 256) norm_backward_kernel<T, W, 256, even><<<parts, 256, 0, s>>>(a);
+  else if (tpr == 1024) norm_backward_kernel<T, W, 1024, even><<<parts, 1024, 0, s>>>(a);
+  else {
+    if (a.partial) norm_columns_kernel<T><<<dim3((unsigned)((a.D + 255) / 256), parts), 256, 0, s>>>(a, parts);
+    norm_backward_loop_kernel<T, W><<<wide_grid(a.rows), kLoopThreads, 0, s>>>(a);
+  }
+}
 template <typename T, typename W>
 hipError_t backward(const NormArgs& a, hipStream_t s) {
-  const int parts = parts_of(a.rows, a.D), tpr = row_threads(a.D);
+  const int parts = parts_of(a.rows, a.D);
   if (a.rows) {
-    if (tpr == 64) norm_backward_kernel<T, W, 64><<<parts, 256, 0, s>>>(a);
-    else if (tpr == 256) norm_backward_kernel<T, W, 256><<<parts, 256, 0, s>>>(a);
-    else if (tpr == 1024) norm_backward_kernel<T, W, 1024><<<parts, 1024, 0, s>>>(a);
-    else {
-      if (a.partial)
-        norm_columns_kernel<T><<<dim3((unsigned)((a.D + 255) / 256), parts), 256, 0, s>>>(a, parts);
-      norm_backward_loop_kernel<T, W><<<wide_grid(a.rows), kLoopThreads, 0, s>>>(a);
-    }
+    if (a.D % vec_of<T>() == 0) backward_as<T, W, true>(a, parts, s);
+    else backward_as<T, W, false>(a, parts, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (a.dw || a.db)
-    norm_sums_kernel<<<dim3((unsigned)((a.D + 63) / 64), 2), 256, 0, s>>>(a.partial, parts, a.D, a.dw, a.db);
+    norm_sums_kernel<<<dim3((unsigned)((a.D + 63) / 64), 2), 1024, 0, s>>>(a.partial, parts, a.D, a.dw, a.db);
   return hipGetLastError();
 }
 

@@ -13,6 +13,7 @@ for arguments that do not fit together, zo.ZoError for what the library refuses.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
@@ -23,14 +24,9 @@ BLOCK = 256     # ZO_ADAMW_BLOCK
 _DTYPES = {torch.float32: zo.FP32, torch.bfloat16: zo.BF16}
 
 
-class _Shape(C.Structure):  # zo_linattn
-    _fields_ = [(n, C.c_int32) for n in ("batch", "length", "q_heads", "kv_heads", "key_dim", "value_dim", "dtype")]
-    _fields_ += [("scale", C.c_float)]
-
-
-class _Heads(C.Structure):  # zo_heads
-    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("position_stride", C.c_int64),
-                ("head_stride", C.c_int64)]
+# zo_linattn and zo_heads, packed (a call passes five of them; ctypes structures take several times as long to fill)
+_SHAPE = struct.Struct("=7if")   # batch, length, q_heads, kv_heads, key_dim, value_dim, dtype, scale
+_HEADS = struct.Struct("=Q3q")   # data, batch_stride, position_stride, head_stride
 
 
 class _Tensor(C.Structure):  # zo_adamw_tensor
@@ -51,7 +47,7 @@ def lib():
     global _lib
     if _lib is None:
         L = zo.lib()
-        vp, shape, heads, i32, i64 = C.c_void_p, C.POINTER(_Shape), C.POINTER(_Heads), C.c_int32, C.c_int64
+        vp, shape, heads, i32, i64 = C.c_void_p, C.c_char_p, C.c_char_p, C.c_int32, C.c_int64
         L.zo_linear_attention_workspace_bytes.argtypes = [shape, i32]
         L.zo_linear_attention_workspace_bytes.restype = C.c_size_t
         L.zo_linear_attention.argtypes = [shape] + [heads] * 4 + [vp] * 5 + [C.c_size_t, vp]
@@ -76,8 +72,16 @@ def _check(st: int):
         zo._check(st)
 
 
-def _stream(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(stream, like: torch.Tensor):
+    """The raw stream of a call on like's device: the given one, or torch's current one."""
+    if stream is not None:
+        return stream.cuda_stream
+    if _current_stream is not None:
+        return _current_stream(like.get_device())
+    return torch.cuda.current_stream(like.device).cuda_stream
 
 
 def _device(t: torch.Tensor, name: str, dtype=None, like: torch.Tensor | None = None):
@@ -86,9 +90,9 @@ def _device(t: torch.Tensor, name: str, dtype=None, like: torch.Tensor | None = 
     if dtype is None:
         if t.dtype not in _DTYPES:
             raise ValueError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    elif t.dtype != dtype:
+    elif t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if like is not None and t.device != like.device:
+    if like is not None and t.get_device() != like.get_device():
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
 
 
@@ -96,7 +100,8 @@ def _flat(t: torch.Tensor | None, name: str, dtype, shape, like: torch.Tensor):
     """The address of a contiguous tensor of a given shape, or None."""
     if t is None:
         return None
-    _device(t, name, dtype, like)
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != like.get_device():
+        _device(t, name, dtype, like)
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     if not t.is_contiguous():
@@ -114,32 +119,32 @@ def _on_stream(stream, *tensors):
 
 # ---- linear attention ----
 
-def _heads(t: torch.Tensor, name: str, shape, like: torch.Tensor) -> _Heads:
-    if not isinstance(t, torch.Tensor) or t.device != like.device:
-        raise ValueError(f"{name} must be a tensor on {like.device}")
-    if t.dtype != like.dtype:
-        raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
+def _heads(t: torch.Tensor, name: str, shape, like: torch.Tensor) -> bytes:
+    """zo_heads of a tensor of a given shape, like's type and device."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not like.dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be a {like.dtype} tensor on {like.device}")
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     st = t.stride()
     if st[-1] != 1 and shape[-1] != 1:
         raise ValueError(f"the values of a head must be contiguous in {name}")
-    return _Heads(t.data_ptr(), st[0], st[1] if len(st) == 4 else 0, st[-2])
+    return _HEADS.pack(t.data_ptr(), st[0], st[1] if len(st) == 4 else 0, st[-2])
 
 
 def _sizes(q, k, v, dims: int, scale):
-    """(shape struct, q's, k's and v's structs) of tensors [B, T, heads, dim], or [B, heads, dim]."""
+    """(B, T, Hq, Hkv, Dk, Dv, zo_linattn, q's, k's and v's zo_heads) of tensors [B, T, heads, dim], or
+    [B, heads, dim]."""
     _device(q, "q")
     if q.dim() != dims or k.dim() != dims or v.dim() != dims:
         raise ValueError(f"q, k and v must have {dims} dimensions")
-    lead = tuple(q.shape[:-2])
-    Hq, Dk = q.shape[-2:]
+    *lead, Hq, Dk = q.shape
     Hkv, Dv = v.shape[-2:]
     if Hkv < 1 or Hq % Hkv:
         raise ValueError(f"{Hq} query heads are no multiple of {Hkv} key/value heads")
-    s = _Shape(lead[0], lead[1] if dims == 4 else 1, Hq, Hkv, Dk, Dv, _DTYPES[q.dtype],
-               Dk ** -0.5 if scale is None else scale)
-    return (s, _heads(q, "q", (*lead, Hq, Dk), q), _heads(k, "k", (*lead, Hkv, Dk), q),
+    B, T = lead[0], lead[1] if dims == 4 else 1
+    return (B, T, Hq, Hkv, Dk, Dv,
+            _SHAPE.pack(B, T, Hq, Hkv, Dk, Dv, _DTYPES[q.dtype], Dk ** -0.5 if scale is None else scale),
+            _heads(q, "q", (*lead, Hq, Dk), q), _heads(k, "k", (*lead, Hkv, Dk), q),
             _heads(v, "v", (*lead, Hkv, Dv), q))
 
 
@@ -158,8 +163,8 @@ def _workspace(given: torch.Tensor | None, need: int, like: torch.Tensor):
 
 def linear_attention_workspace_bytes(B: int, T: int, q_heads: int, kv_heads: int, key_dim: int, value_dim: int,
                                      dtype=torch.float32, backward: bool = False) -> int:
-    s = _Shape(B, T, q_heads, kv_heads, key_dim, value_dim, _DTYPES[dtype], 1.0)
-    return int(lib().zo_linear_attention_workspace_bytes(C.byref(s), int(backward)))
+    s = _SHAPE.pack(B, T, q_heads, kv_heads, key_dim, value_dim, _DTYPES[dtype], 1.0)
+    return int(lib().zo_linear_attention_workspace_bytes(s, int(backward)))
 
 
 def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
@@ -174,19 +179,17 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     [B, Hkv, Dk, Dv]; lengths int32 [B] or None (all T). The final state is returned with
     return_state, or written into final_state (which may be initial_state)."""
     L = lib()
-    s, hq, hk, hv = _sizes(q, k, v, 4, scale)
-    B, T, Hkv = s.batch, s.length, s.kv_heads
-    states = (B, Hkv, s.key_dim, s.value_dim)
-    o = torch.empty((B, T, s.q_heads, s.value_dim), dtype=q.dtype, device=q.device) if out is None else out
-    if final_state is None and return_state:
-        final_state = torch.empty(states, dtype=torch.float32, device=q.device)
+    B, T, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 4, scale)
+    states = (B, Hkv, Dk, Dv)
+    o = torch.empty((B, T, Hq, Dv), dtype=q.dtype, device=q.device) if out is None else out
     f32 = torch.float32
-    ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(C.byref(s), 0), q)
+    if final_state is None and return_state:
+        final_state = torch.empty(states, dtype=f32, device=q.device)
+    ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(s, 0), q)
     _check(L.zo_linear_attention(
-        C.byref(s), C.byref(hq), C.byref(hk), C.byref(hv),
-        C.byref(_heads(o, "out", (B, T, s.q_heads, s.value_dim), q)), _flat(log_decay, "log_decay", f32, (Hkv,), q),
+        s, hq, hk, hv, _heads(o, "out", (B, T, Hq, Dv), q), _flat(log_decay, "log_decay", f32, (Hkv,), q),
         _flat(lengths, "lengths", torch.int32, (B,), q), _flat(initial_state, "initial_state", f32, states, q),
-        _flat(final_state, "final_state", f32, states, q), wp, wn, _stream(stream)))
+        _flat(final_state, "final_state", f32, states, q), wp, wn, _stream(stream, q)))
     _on_stream(stream, o, final_state, ws)
     return o, final_state
 
@@ -201,24 +204,22 @@ def linear_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor
     [B, T, Hq, Dv] and the final state's dfinal_state (None: zeros), asynchronously.
     The initial state's gradient is computed when one was given, or as return_dinitial says."""
     L = lib()
-    s, hq, hk, hv = _sizes(q, k, v, 4, scale)
-    B, T, Hq, Hkv, Dk, Dv = s.batch, s.length, s.q_heads, s.kv_heads, s.key_dim, s.value_dim
+    B, T, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 4, scale)
     states = (B, Hkv, Dk, Dv)
     dq = torch.empty((B, T, Hq, Dk), dtype=q.dtype, device=q.device) if dq is None else dq
     dk = torch.empty((B, T, Hkv, Dk), dtype=q.dtype, device=q.device) if dk is None else dk
     dv = torch.empty((B, T, Hkv, Dv), dtype=q.dtype, device=q.device) if dv is None else dv
     if return_dinitial is None:
         return_dinitial = initial_state is not None
-    dinitial = torch.empty(states, dtype=torch.float32, device=q.device) if return_dinitial else None
     f32 = torch.float32
-    ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(C.byref(s), 1), q)
+    dinitial = torch.empty(states, dtype=f32, device=q.device) if return_dinitial else None
+    ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(s, 1), q)
     _check(L.zo_linear_attention_backward(
-        C.byref(s), C.byref(_heads(do, "do", (B, T, Hq, Dv), q)), C.byref(hq), C.byref(hk), C.byref(hv),
-        C.byref(_heads(dq, "dq", (B, T, Hq, Dk), q)), C.byref(_heads(dk, "dk", (B, T, Hkv, Dk), q)),
-        C.byref(_heads(dv, "dv", (B, T, Hkv, Dv), q)), _flat(log_decay, "log_decay", f32, (Hkv,), q),
-        _flat(lengths, "lengths", torch.int32, (B,), q), _flat(initial_state, "initial_state", f32, states, q),
-        _flat(dfinal_state, "dfinal_state", f32, states, q), _flat(dinitial, "dinitial", f32, states, q), wp, wn,
-        _stream(stream)))
+        s, _heads(do, "do", (B, T, Hq, Dv), q), hq, hk, hv, _heads(dq, "dq", (B, T, Hq, Dk), q),
+        _heads(dk, "dk", (B, T, Hkv, Dk), q), _heads(dv, "dv", (B, T, Hkv, Dv), q),
+        _flat(log_decay, "log_decay", f32, (Hkv,), q), _flat(lengths, "lengths", torch.int32, (B,), q),
+        _flat(initial_state, "initial_state", f32, states, q), _flat(dfinal_state, "dfinal_state", f32, states, q),
+        _flat(dinitial, "dinitial", f32, states, q), wp, wn, _stream(stream, q)))
     _on_stream(stream, dq, dk, dv, dinitial, ws)
     return dq, dk, dv, dinitial
 
@@ -231,18 +232,17 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     [B], no two alike) names each sequence's state in it, -1 a sequence without one (its
     output is zero); None: sequence b's is state[b]."""
     L = lib()
-    s, hq, hk, hv = _sizes(q, k, v, 3, scale)
-    B, Hkv = s.batch, s.kv_heads
-    if state.dim() != 4 or state.shape[0] > 0x7fffffff:
-        raise ValueError("state must be [n, Hkv, Dk, Dv]")
+    B, _, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 3, scale)
     n = state.shape[0]
-    o = torch.empty((B, s.q_heads, s.value_dim), dtype=q.dtype, device=q.device) if out is None else out
+    if n > 0x7fffffff:
+        raise ValueError("state must hold fewer than 2^31 states")
+    o = torch.empty((B, Hq, Dv), dtype=q.dtype, device=q.device) if out is None else out
     _check(L.zo_linear_attention_step(
-        C.byref(s), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(_heads(o, "out", (B, s.q_heads, s.value_dim), q)),
-        _flat(log_decay, "log_decay", torch.float32, (Hkv,), q),
-        _flat(state, "state", torch.float32, (n, Hkv, s.key_dim, s.value_dim), q), n,
-        _flat(slots, "slots", torch.int32, (B,), q), _stream(stream)))
-    _on_stream(stream, o)
+        s, hq, hk, hv, _heads(o, "out", (B, Hq, Dv), q), _flat(log_decay, "log_decay", torch.float32, (Hkv,), q),
+        _flat(state, "state", torch.float32, (n, Hkv, Dk, Dv), q), n, _flat(slots, "slots", torch.int32, (B,), q),
+        _stream(stream, q)))
+    if stream is not None:
+        _on_stream(stream, o)
     return o
 
 
@@ -283,14 +283,15 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     L = lib()
     rows, D, xs = _rows(x, "x")
     wtype, w, b = _norm_params(weight, bias, D, x)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    dev = x.device
+    y = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
     ys = D if out is None else _rows(y, "out", x.shape, x)[2]
-    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-    sp = stats.data_ptr()
-    _check(L.zo_layer_norm(_DTYPES[x.dtype], wtype, rows, D, x.data_ptr(), xs, w, b, eps, y.data_ptr(), ys, sp,
-                           sp + 4 * rows, _stream(stream)))
-    _on_stream(stream, y, stats)
-    return y, stats[0], stats[1]
+    mean = torch.empty(rows, dtype=torch.float32, device=dev)
+    rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+    _check(L.zo_layer_norm(_DTYPES[x.dtype], wtype, rows, D, x.data_ptr(), xs, w, b, eps, y.data_ptr(), ys,
+                           mean.data_ptr(), rstd.data_ptr(), _stream(stream, x)))
+    _on_stream(stream, y, mean, rstd)
+    return y, mean, rstd
 
 
 def layer_norm_workspace_bytes(rows: int, D: int) -> int:
@@ -308,15 +309,16 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
     wtype, w, _ = _norm_params(weight, None, D, x)
     mp = _flat(mean, "mean", torch.float32, (rows,), x)
     rp = _flat(rstd, "rstd", torch.float32, (rows,), x)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    dev = x.device
+    dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
     dxs = D if out is None else _rows(dx, "out", x.shape, x)[2]
-    dw = torch.empty((2, D), dtype=torch.float32, device=x.device)
-    dp = dw.data_ptr()
+    dw = torch.empty(D, dtype=torch.float32, device=dev)
+    db = torch.empty(D, dtype=torch.float32, device=dev)
     ws, wp, wn = _workspace(workspace, L.zo_layer_norm_workspace_bytes(rows, D), x)
     _check(L.zo_layer_norm_backward(_DTYPES[x.dtype], wtype, rows, D, dy.data_ptr(), dys, x.data_ptr(), xs, w, mp, rp,
-                                    dx.data_ptr(), dxs, dp, dp + 4 * D, wp, wn, _stream(stream)))
-    _on_stream(stream, dx, dw, ws)
-    return dx, dw[0], dw[1]
+                                    dx.data_ptr(), dxs, dw.data_ptr(), db.data_ptr(), wp, wn, _stream(stream, x)))
+    _on_stream(stream, dx, dw, db, ws)
+    return dx, dw, db
 
 
 # ---- AdamW ----
@@ -374,20 +376,21 @@ class AdamW:
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} tensors")
-        dev = self.m.device
-        for t, p, shape, g in zip(self._table, self.params, self._shapes, grads):
-            if g.device != dev or g.shape != shape or not g.is_contiguous() or g.dtype not in _DTYPES:
-                raise ValueError(f"gradients must be contiguous fp32 or bf16 tensors of their parameters' shapes on "
-                                 f"{dev}: got {g.dtype} {list(g.shape)} on {g.device} for {list(shape)}")
-            t.param, t.grad, t.gdtype = p.data_ptr(), g.data_ptr(), _DTYPES[g.dtype]
         like = self.m
+        dev = like.get_device()
+        for t, p, shape, g in zip(self._table, self.params, self._shapes, grads):
+            kind = _DTYPES.get(g.dtype)
+            if kind is None or g.get_device() != dev or g.shape != shape or not g.is_contiguous():
+                raise ValueError(f"gradients must be contiguous fp32 or bf16 tensors of their parameters' shapes on "
+                                 f"{like.device}: got {g.dtype} {list(g.shape)} on {g.device} for {list(shape)}")
+            t.param, t.grad, t.gdtype = p.data_ptr(), g.data_ptr(), kind
         gs = _flat(grad_scale, "grad_scale", torch.float32, (1,), like)
         sk = _flat(skipped, "skipped", torch.int32, (1,), like)
         cfg = _AdamWConfig(self.lr, self.betas[0], self.betas[1], self.eps, self.step_count + 1, self.state_bits)
         eight = self.state_bits == 8
         _check(lib().zo_adamw(C.byref(cfg), self._table, len(grads), self.m.data_ptr(), self.v.data_ptr(),
                               self.m_scale.data_ptr() if eight else None, self.v_scale.data_ptr() if eight else None,
-                              gs, sk, _stream(stream)))
+                              gs, sk, _stream(stream, like)))
         self.step_count += 1
 
     def moments(self, stream=None):
@@ -397,6 +400,6 @@ class AdamW:
         m = torch.empty(self.m.numel(), dtype=torch.float32, device=self.m.device)
         v = torch.empty_like(m)
         _check(lib().zo_adamw_moments(m.numel(), self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr(),
-                                      self.v_scale.data_ptr(), m.data_ptr(), v.data_ptr(), _stream(stream)))
+                                      self.v_scale.data_ptr(), m.data_ptr(), v.data_ptr(), _stream(stream, m)))
         _on_stream(stream, m, v)
         return m, v

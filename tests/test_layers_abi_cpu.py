@@ -47,16 +47,16 @@ def test_header_is_c(tmp_path):
 def shape(layers, **kw):
     s = dict(batch=2, length=8, q_heads=4, kv_heads=2, key_dim=32, value_dim=32, dtype=0, scale=1.0)
     s.update(kw)
-    return layers._Shape(*s.values())
+    return layers._SHAPE.pack(*s.values())
 
 
 def heads(layers, data=FAKE):
-    return C.byref(layers._Heads(data, 1, 1, 1))
+    return layers._HEADS.pack(data or 0, 1, 1, 1)
 
 
 def attention(layers, s, data=FAKE, decay=FAKE, lengths=None, initial=None, final=None, ws=FAKE, wn=1 << 40):
     h = heads(layers, data)
-    return layers.lib().zo_linear_attention(C.byref(s), h, h, h, h, decay, lengths, initial, final, ws, wn, None)
+    return layers.lib().zo_linear_attention(s, h, h, h, h, decay, lengths, initial, final, ws, wn, None)
 
 
 def error():
@@ -75,10 +75,10 @@ def test_linear_attention_shapes_are_refused(layers, bad, status, word):
     L, h = layers.lib(), heads(layers)
     s = shape(layers, **bad)
     assert attention(layers, s) == status and word in error()
-    assert L.zo_linear_attention_backward(C.byref(s), h, h, h, h, h, h, h, FAKE, None, None, None, None, FAKE, 1 << 40,
+    assert L.zo_linear_attention_backward(s, h, h, h, h, h, h, h, FAKE, None, None, None, None, FAKE, 1 << 40,
                                           None) == status
-    assert L.zo_linear_attention_step(C.byref(s), h, h, h, h, FAKE, FAKE, 1 << 30, None, None) == status
-    assert L.zo_linear_attention_workspace_bytes(C.byref(s), 0) == 0
+    assert L.zo_linear_attention_step(s, h, h, h, h, FAKE, FAKE, 1 << 30, None, None) == status
+    assert L.zo_linear_attention_workspace_bytes(s, 0) == 0
 
 
 def test_linear_attention_pointers_are_refused(layers):
@@ -89,16 +89,16 @@ def test_linear_attention_pointers_are_refused(layers):
     for name in ("decay", "lengths", "initial", "final"):
         assert attention(layers, s, **{name: FAKE + 2}) == -1 and "aligned" in error()
     assert attention(layers, s, ws=FAKE + 8) == -1 and "workspace" in error()
-    assert L.zo_linear_attention(C.byref(s), None, h, h, h, FAKE, None, None, None, FAKE, 1 << 40, None) == -1
+    assert L.zo_linear_attention(s, None, h, h, h, FAKE, None, None, None, FAKE, 1 << 40, None) == -1
     assert L.zo_linear_attention(None, h, h, h, h, FAKE, None, None, None, FAKE, 1 << 40, None) == -1
-    assert L.zo_linear_attention_backward(C.byref(s), h, h, h, None, h, h, h, FAKE, None, None, None, None, FAKE,
+    assert L.zo_linear_attention_backward(s, h, h, h, None, h, h, h, FAKE, None, None, None, None, FAKE,
                                           1 << 40, None) == -1
     step = L.zo_linear_attention_step
-    assert step(C.byref(s), h, h, h, h, FAKE, FAKE, 1, None, None) == -1 and "n_slots" in error()
-    assert step(C.byref(s), h, h, h, h, FAKE, FAKE, -1, FAKE, None) == -1
-    assert step(C.byref(s), h, h, h, h, FAKE, None, 4, None, None) == -1
-    assert step(C.byref(s), h, h, h, h, FAKE, FAKE, 4, FAKE + 1, None) == -1 and "slots" in error()
-    need = L.zo_linear_attention_workspace_bytes(C.byref(shape(layers, batch=1, length=1 << 16, dtype=1)), 0)
+    assert step(s, h, h, h, h, FAKE, FAKE, 1, None, None) == -1 and "n_slots" in error()
+    assert step(s, h, h, h, h, FAKE, FAKE, -1, FAKE, None) == -1
+    assert step(s, h, h, h, h, FAKE, None, 4, None, None) == -1
+    assert step(s, h, h, h, h, FAKE, FAKE, 4, FAKE + 1, None) == -1 and "slots" in error()
+    need = L.zo_linear_attention_workspace_bytes(shape(layers, batch=1, length=1 << 16, dtype=1), 0)
     if need:
         big = shape(layers, batch=1, length=1 << 16, dtype=1)
         assert attention(layers, big, wn=need - 1) == -4 and attention(layers, big, ws=None, wn=need) == -1
