@@ -57,7 +57,6 @@ constexpr int kXcds = 8;
 constexpr int kParts = 3;     // bf16 parts of the decayed z in the state's sum
 
 typedef float f4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
@@ -112,12 +111,6 @@ struct Op<float> {
   }
 };
 
-// 16 bytes at p, which is aligned to its type.
-template <typename T>
-__device__ __forceinline__ u4 load16(const T* p) {
-  struct __attribute__((packed, aligned(sizeof(T)))) Any { u4 v; };
-  return ((const Any*)p)->v;
-}
 // The first d (fewer than 16 bytes hold) values of a row, then zeros.
 template <typename T>
 __device__ __forceinline__ u4 load_few(const T* p, int d) {
@@ -130,20 +123,6 @@ __device__ __forceinline__ u4 load_few(const T* p, int d) {
     }
   return v;
 }
-// Drops the first n values (fewer than 16 bytes hold), zeros after the rest: the end of a row,
-// read with the 16 bytes that end there.
-template <typename T>
-__device__ __forceinline__ u4 drop(u4 v, int n) {
-  int words = n;
-  if constexpr (sizeof(T) == 2) {
-    words = n >> 1;
-    if (n & 1) v = u4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
-  }
-  if (words & 1) v = u4{v[1], v[2], v[3], 0};
-  if (words & 2) v = u4{v[2], v[3], 0, 0};
-  return v;
-}
-
 // Gathers, over words of values, the sign bit of each whose exponent is all ones.
 template <typename T>
 __device__ __forceinline__ uint32_t not_finite(u4 v) {

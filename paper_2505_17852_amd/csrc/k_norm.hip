@@ -63,25 +63,24 @@ constexpr int vals_of() { return TPR > 256 ? 8 : 16; }
 template <typename T>
 constexpr int vec_of() { return sizeof(T) == 2 ? 8 : 4; }
 
-// A row as it lies in memory, on its way to a thread's registers. even: D is a multiple of VEC, and runs past
-// the end repeat the last one (no branch around a load: the next row's loads stay in flight while
-// this one is worked on).
-template <typename T, int TPR, bool even, int VEC = vec_of<T>()>
+// A row as it lies in memory, on its way to a thread's registers, 16 bytes a run. No branch stands around a load, so
+// that the next row's loads stay in flight while this one is worked on: runs past the end repeat the
+// last 16 bytes, and the run that the row ends in (D not a multiple of VEC) is the last 16 bytes,
+// moved down when it is used. D is VEC at least, but for short rows.
+template <typename T, int TPR, bool even>
 struct RawRow {
-  static constexpr int N = vals_of<TPR>() / VEC;
-  Run<T, VEC> v[N];
+  static constexpr int VEC = vec_of<T>(), N = vals_of<TPR>() / VEC;
+  u4 v[N];
   __device__ __forceinline__ void load(const T* p, int lane, int D) {
+    if (even || D >= VEC) {
 #pragma unroll
-    for (int c = 0; c < N; ++c) {
-      const int j = (c * TPR + lane) * VEC;
-      if constexpr (even) {
-        v[c] = *(const Run<T, VEC>*)(p + min(j, D - VEC));
-      } else if (j + VEC <= D) {
-        v[c] = *(const Run<T, VEC>*)(p + j);
-      } else {
+      for (int c = 0; c < N; ++c) v[c] = load16(p + min((c * TPR + lane) * VEC, D - VEC));
+    } else {
+      T few[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[c].v[e] = p[min(j + e, D - 1)];
-      }
+      for (int e = 0; e < VEC; ++e) few[e] = p[min(e, D - 1)];
+#pragma unroll
+      for (int c = 0; c < N; ++c) v[c] = __builtin_bit_cast(u4, few);
     }
   }
   // fp32, zeros past the row's end
@@ -89,16 +88,29 @@ struct RawRow {
 #pragma unroll
     for (int c = 0; c < N; ++c) {
       const int j = (c * TPR + lane) * VEC;
+      u4 run = v[c];
+      if constexpr (!even) run = drop<T>(run, D >= VEC ? min(max(j - (D - VEC), 0), VEC - 1) : 0);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) out[c * VEC + e] = (even ? j : j + e) < D ? to_f32(v[c].v[e]) : 0.0f;
+      for (int e = 0; e < VEC; ++e) {
+        const uint32_t word = sizeof(T) == 4 ? run[e] : e & 1 ? run[e / 2] & 0xffff0000u : run[e / 2] << 16;
+        out[c * VEC + e] = (even ? j : j + e) < D ? __uint_as_float(word) : 0.0f;
+      }
     }
   }
 };
-template <typename T, int TPR, bool even, int VEC>
+// Weights, read once per workgroup, in the runs of x.
+template <typename T, int TPR, int VEC>
 __device__ __forceinline__ void load_row(const T* p, int lane, int D, float* out) {
-  RawRow<T, TPR, even, VEC> r;
-  r.load(p, lane, D);
-  r.get(lane, D, out);
+#pragma unroll
+  for (int c = 0; c < vals_of<TPR>() / VEC; ++c) {
+    const int j = (c * TPR + lane) * VEC;
+    if (j + VEC <= D) {
+      load_run<T, VEC>(p + j, out + c * VEC);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) out[c * VEC + e] = j + e < D ? to_f32(p[j + e]) : 0.0f;
+    }
+  }
 }
 
 template <typename T, int TPR, int VEC>
@@ -138,8 +150,8 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_kernel(NormArgs a) {
     w[i] = 1.0f;
     b[i] = 0.0f;
   }
-  if (a.w) load_row<W, TPR, even, VEC>((const W*)a.w, lane, D, w);
-  if (a.b) load_row<W, TPR, even, VEC>((const W*)a.b, lane, D, b);
+  if (a.w) load_row<W, TPR, VEC>((const W*)a.w, lane, D, w);
+  if (a.b) load_row<W, TPR, VEC>((const W*)a.b, lane, D, b);
   for (; r < a.rows; r += step) {
     float x[kVals];
     raw.get(lane, D, x);
@@ -195,7 +207,7 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormAr
     dw[i] = 0.0f;
     db[i] = 0.0f;
   }
-  if (a.w) load_row<W, TPR, even, VEC>((const W*)a.w, lane, D, w);
+  if (a.w) load_row<W, TPR, VEC>((const W*)a.w, lane, D, w);
   int turn = 0;
   for (; r < a.rows; r += step) {
     float x[kVals], dy[kVals];

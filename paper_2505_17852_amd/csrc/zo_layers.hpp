@@ -59,6 +59,27 @@ __device__ __forceinline__ void store_run(T* p, const float* in) {
   }
 }
 
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+// 16 bytes at p, which is aligned to its type.
+template <typename T>
+__device__ __forceinline__ u4 load16(const T* p) {
+  struct __attribute__((packed, aligned(sizeof(T)))) Any { u4 v; };
+  return ((const Any*)p)->v;
+}
+// Drops the first n values (fewer than 16 bytes hold), zeros after the rest: the end of a row,
+// read with the 16 bytes that end there.
+template <typename T>
+__device__ __forceinline__ u4 drop(u4 v, int n) {
+  int words = n;
+  if constexpr (sizeof(T) == 2) {
+    words = n >> 1;
+    if (n & 1) v = u4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+  }
+  if (words & 1) v = u4{v[1], v[2], v[3], 0};
+  if (words & 2) v = u4{v[2], v[3], 0, 0};
+  return v;
+}
+
 // ---- linear attention (k_linattn.hip, k_linattn_step.hip) ----
 
 struct Heads {
