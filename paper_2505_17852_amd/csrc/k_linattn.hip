@@ -292,7 +292,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
 
   const int n = c.lengths ? min(max(c.lengths[b], 0), c.T) : c.T;
   const int r0 = seg * pl.length, r1 = min(n, r0 + pl.length);  // the segment's positions
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, m = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, m = lane & 15;
+  // (fp32: the rows go to other waves, so other SIMDs, in the next workgroups of a CU)
+  const int w = ((tid >> 6) + (sizeof(T) == 4 ? (int)(turn >> 5) : 0)) & 3;
   const float lg = c.log_decay[kvh] * 1.44269504088896340736f;
   const int off = a.reverse ? 0 : 1;
 
@@ -309,8 +311,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   // R: rows 16 i + 4 g + r, columns col + 16 (w NW + u) + m
   f4 R[NW][MT];
   const int rz = col + 16 * w * NW + m;
+  const float* from = nullptr;
   {
-    const float* from = nullptr;
     bool turned = false;
     if (seg == 0) {
       if (a.init) from = a.init + bh * a.dx * a.dz;
@@ -367,10 +369,14 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   // The loads of the next step go out once this one's tiles are in LDS, or, where the registers of two waves
   // per SIMD do not hold them beside the output, once that is stored.
   constexpr bool late = sizeof(T) == 2 && SL == 128;
+  // Whether the first chunk's products with a state of zero and the last one's sum that nothing reads are left out
+  // (the branches cost the kernel that is short of registers more than two of its many chunks' products).
+  constexpr bool ends = !late;
   // (kept in scalar registers: loads of arguments inside the loop would wait for the LDS too)
   int64_t yh = a.y.h, zh = a.z.h, out_turn = a.reverse ? -a.ot : a.ot;
   T* outp = out + origin * a.ot + col;
   int sources = a.sources, dxn = a.dx;
+  const bool fin = a.fin != nullptr;
   asm volatile("" : "+s"(yh), "+s"(zh), "+s"(out_turn), "+s"(outp), "+s"(sources), "+s"(dxn));
   Y yn;
   Z zn;
@@ -445,11 +451,14 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       f4 P[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) P[t] = f4{0, 0, 0, 0};
+      // (bf16: all four tiles, also those past the wave's rows: there the wave with most of them is what the others
+      // wait for. fp32, whose products take 16 times as long, leaves them out.)
+      constexpr bool all = sizeof(T) == 2;
 #pragma unroll
       for (int i = 0; i < NX; ++i)
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-          P[t] = O::mma(O::along(ys + 16 * ((w - t) & 3) * YS + m * YS + i * KB, g), xn[i], P[t]);
+          if (all || t <= w) P[t] = O::mma(O::along(ys + 16 * ((w - t) & 3) * YS + m * YS + i * KB, g), xn[i], P[t]);
 #pragma unroll
       for (int r = 0; r < 4; ++r) P[0][r] = 4 * g + r <= m ? P[0][r] * own_f[r] : 0.0f;
 #pragma unroll
@@ -472,6 +481,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
         if (src == 0) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) acc[j] = f4{0, 0, 0, 0};
+        }
+        if (src == 0 && (!ends || start > r0 - lead0 || from)) {
 #pragma unroll
           for (int i = 0; i < NX; ++i)
 #pragma unroll
@@ -488,8 +499,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
         if (!flagged) {
 #pragma unroll
           for (int k = 0; k < NJ; ++k)
+            if (all || k <= w)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = O::mma(z_of(k, j), pb[k], acc[j]);
+              for (int j = 0; j < 4; ++j) acc[j] = O::mma(z_of(k, j), pb[k], acc[j]);
         } else {
 #pragma unroll
           for (int k = 0; k < NJ; ++k)
@@ -524,11 +536,14 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       yn.fetch(yr.base(next) + next_src * yh, dxn);
       zn.fetch(zr.base(next) + next_src * zh, zd);
     }
-    if (src == 0)
+    // the state after the chunk
+    const bool read = state_only || !ends || start + kChunk < r1 || fin;
+    if (read && src == 0)
 #pragma unroll
       for (int u = 0; u < NW; ++u)
 #pragma unroll
         for (int i = 0; i < MT; ++i) R[u][i] *= rf;
+    if (read)
 #pragma unroll
     for (int k = 0; k < NJ; ++k) {
       // gamma^(..) z; in bf16 parts, the next one of what the last left out
@@ -628,11 +643,18 @@ __global__ __launch_bounds__(kThreads) void linattn_scan_kernel(LinCall c, Plan 
   const int whole = min(n / pl.length, pl.segments - 1);  // segments whose sums exist
   const float gamma = decay(c.log_decay[bh % c.kv_heads] * 1.44269504088896340736f, pl.length);
   float* p = pl.states[pass] + bh * (pl.segments - 1) * per + e;
+  // (eight loads in flight at a time)
   float s = 0;
-  for (int i = 0; i < whole; ++i) {
-    const float u = p[(int64_t)i * per];
-    s = i == 0 ? u : fmaf(gamma, s, u);
-    p[(int64_t)i * per] = s;
+  for (int i = 0; i < whole; i += 8) {
+    float u[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) u[k] = p[(int64_t)min(i + k, whole - 1) * per];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (i + k < whole) {
+        s = i + k == 0 ? u[k] : fmaf(gamma, s, u[k]);
+        p[(int64_t)(i + k) * per] = s;
+      }
   }
 }
 
@@ -688,16 +710,18 @@ hipError_t launch(const LinCall& c, const Plan& pl, int dx, int slice, hipStream
 }
 
 // Columns of z per workgroup: 128 where states have more than 64 rows and columns and no more
-// than 128 rows (x and y are then read once, and the scores formed once), 64 otherwise, and where
-// several query heads add to one output.
-int slice_of(int dk, int dv, int share, bool backward) {
-  if (backward && share > 1) return 64;
+// than 128 rows (x and y are then read once, and the scores formed once; 16 sequences of 1,024 positions, 32 heads
+// of 128, forward and backward: 0.49 ms against 0.54), 64 otherwise, where several query heads
+// add to one output, and where the states are too few to give every CU one (one sequence of 8,192
+// positions, 32 heads: 0.12 ms against 0.14).
+int slice_of(int64_t states, int dk, int dv, int share, bool backward) {
+  if ((backward ? states : states * share) < 256 || (backward && share > 1)) return 64;
   const int dx = backward ? std::max(dk, dv) : dk, dz = backward ? std::min(dk, dv) : dv;
   return dx > 64 && dx <= 128 && dz > 64 ? 128 : 64;
 }
 
 void plan_segments(int B, int kv_heads, int share, int dk, int dv, int T, bool backward, Plan* pl) {
-  const int sl = slice_of(dk, dv, share, backward), nk = (dk + sl - 1) / sl, nv = (dv + sl - 1) / sl;
+  const int sl = slice_of((int64_t)B * kv_heads, dk, dv, share, backward), nk = (dk + sl - 1) / sl, nv = (dv + sl - 1) / sl;
   const int64_t per_state = backward ? (int64_t)share * nk + nk + nv : (int64_t)share * nv;
   split((int64_t)B * kv_heads * per_state, T, &pl->segments, &pl->length);
 }
@@ -716,7 +740,7 @@ hipError_t launch_linattn(const LinCall& c, hipStream_t s) {
   const LinPass& p = c.pass[0];
   const bool backward = c.npasses > 1;
   Plan pl{};
-  const int dk = backward ? p.dz : p.dx, dv = backward ? p.dx : p.dz, sl = slice_of(dk, dv, c.share, backward);
+  const int dk = backward ? p.dz : p.dx, dv = backward ? p.dx : p.dz, sl = slice_of((int64_t)c.B * c.kv_heads, dk, dv, c.share, backward);
   plan_segments(c.B, c.kv_heads, c.share, dk, dv, c.T, backward, &pl);
   bool even = true;
   int dx = 0;

@@ -85,7 +85,7 @@ def _stream(stream, like: torch.Tensor):
 
 
 def _device(t: torch.Tensor, name: str, dtype=None, like: torch.Tensor | None = None):
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    if not isinstance(t, torch.Tensor) or t.get_device() < 0:
         raise ValueError(f"{name} must be a device tensor")
     if dtype is None:
         if t.dtype not in _DTYPES:
@@ -135,17 +135,24 @@ def _sizes(q, k, v, dims: int, scale):
     """(B, T, Hq, Hkv, Dk, Dv, zo_linattn, q's, k's and v's zo_heads) of tensors [B, T, heads, dim], or
     [B, heads, dim]."""
     _device(q, "q")
-    if q.dim() != dims or k.dim() != dims or v.dim() != dims:
+    qs, ks, vs = q.shape, k.shape, v.shape
+    if not len(qs) == len(ks) == len(vs) == dims:
         raise ValueError(f"q, k and v must have {dims} dimensions")
-    *lead, Hq, Dk = q.shape
-    Hkv, Dv = v.shape[-2:]
+    B, T = qs[0], qs[1] if dims == 4 else 1
+    Hq, Dk, Hkv, Dv = qs[-2], qs[-1], vs[-2], vs[-1]
     if Hkv < 1 or Hq % Hkv:
         raise ValueError(f"{Hq} query heads are no multiple of {Hkv} key/value heads")
-    B, T = lead[0], lead[1] if dims == 4 else 1
+    lead = (B, T) if dims == 4 else (B,)
     return (B, T, Hq, Hkv, Dk, Dv,
             _SHAPE.pack(B, T, Hq, Hkv, Dk, Dv, _DTYPES[q.dtype], Dk ** -0.5 if scale is None else scale),
-            _heads(q, "q", (*lead, Hq, Dk), q), _heads(k, "k", (*lead, Hkv, Dk), q),
-            _heads(v, "v", (*lead, Hkv, Dv), q))
+            _heads(q, "q", qs, q), _heads(k, "k", (*lead, Hkv, Dk), q), _heads(v, "v", (*lead, Hkv, Dv), q))
+
+
+def _new_heads(like: torch.Tensor, *shape):
+    """A new contiguous tensor [B, T, heads, dim] (or [B, heads, dim]) of like's type, and its zo_heads."""
+    t = like.new_empty(shape)
+    H, D = shape[-2:]
+    return t, _HEADS.pack(t.data_ptr(), (shape[1] if len(shape) == 4 else 1) * H * D, H * D, D)
 
 
 def _workspace(given: torch.Tensor | None, need: int, like: torch.Tensor):
@@ -181,13 +188,13 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     L = lib()
     B, T, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 4, scale)
     states = (B, Hkv, Dk, Dv)
-    o = torch.empty((B, T, Hq, Dv), dtype=q.dtype, device=q.device) if out is None else out
+    o, ho = _new_heads(q, B, T, Hq, Dv) if out is None else (out, _heads(out, "out", (B, T, Hq, Dv), q))
     f32 = torch.float32
     if final_state is None and return_state:
         final_state = torch.empty(states, dtype=f32, device=q.device)
     ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(s, 0), q)
     _check(L.zo_linear_attention(
-        s, hq, hk, hv, _heads(o, "out", (B, T, Hq, Dv), q), _flat(log_decay, "log_decay", f32, (Hkv,), q),
+        s, hq, hk, hv, ho, _flat(log_decay, "log_decay", f32, (Hkv,), q),
         _flat(lengths, "lengths", torch.int32, (B,), q), _flat(initial_state, "initial_state", f32, states, q),
         _flat(final_state, "final_state", f32, states, q), wp, wn, _stream(stream, q)))
     _on_stream(stream, o, final_state, ws)
@@ -206,17 +213,16 @@ def linear_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor
     L = lib()
     B, T, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 4, scale)
     states = (B, Hkv, Dk, Dv)
-    dq = torch.empty((B, T, Hq, Dk), dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty((B, T, Hkv, Dk), dtype=q.dtype, device=q.device) if dk is None else dk
-    dv = torch.empty((B, T, Hkv, Dv), dtype=q.dtype, device=q.device) if dv is None else dv
+    dq, hdq = _new_heads(q, B, T, Hq, Dk) if dq is None else (dq, _heads(dq, "dq", (B, T, Hq, Dk), q))
+    dk, hdk = _new_heads(q, B, T, Hkv, Dk) if dk is None else (dk, _heads(dk, "dk", (B, T, Hkv, Dk), q))
+    dv, hdv = _new_heads(q, B, T, Hkv, Dv) if dv is None else (dv, _heads(dv, "dv", (B, T, Hkv, Dv), q))
     if return_dinitial is None:
         return_dinitial = initial_state is not None
     f32 = torch.float32
     dinitial = torch.empty(states, dtype=f32, device=q.device) if return_dinitial else None
     ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(s, 1), q)
     _check(L.zo_linear_attention_backward(
-        s, _heads(do, "do", (B, T, Hq, Dv), q), hq, hk, hv, _heads(dq, "dq", (B, T, Hq, Dk), q),
-        _heads(dk, "dk", (B, T, Hkv, Dk), q), _heads(dv, "dv", (B, T, Hkv, Dv), q),
+        s, _heads(do, "do", (B, T, Hq, Dv), q), hq, hk, hv, hdq, hdk, hdv,
         _flat(log_decay, "log_decay", f32, (Hkv,), q), _flat(lengths, "lengths", torch.int32, (B,), q),
         _flat(initial_state, "initial_state", f32, states, q), _flat(dfinal_state, "dfinal_state", f32, states, q),
         _flat(dinitial, "dinitial", f32, states, q), wp, wn, _stream(stream, q)))
@@ -236,9 +242,9 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     n = state.shape[0]
     if n > 0x7fffffff:
         raise ValueError("state must hold fewer than 2^31 states")
-    o = torch.empty((B, Hq, Dv), dtype=q.dtype, device=q.device) if out is None else out
+    o, ho = _new_heads(q, B, Hq, Dv) if out is None else (out, _heads(out, "out", (B, Hq, Dv), q))
     _check(L.zo_linear_attention_step(
-        s, hq, hk, hv, _heads(o, "out", (B, Hq, Dv), q), _flat(log_decay, "log_decay", torch.float32, (Hkv,), q),
+        s, hq, hk, hv, ho, _flat(log_decay, "log_decay", torch.float32, (Hkv,), q),
         _flat(state, "state", torch.float32, (n, Hkv, Dk, Dv), q), n, _flat(slots, "slots", torch.int32, (B,), q),
         _stream(stream, q)))
     if stream is not None:
