@@ -1,0 +1,198 @@
+"""A recurrent language model with linear attention, trained by exact gradients.
+
+The first-order counterpart of `train`: the same workloads (tokens, masks, model
+sizes), with blocks of linear attention in place of the LSTM layers,
+
+    h = h + Wo attention(norm(h) Wqkv)        (n_layers times)
+    logits = norm(h) Wout^T + b
+
+whose whole sequences run in parallel over the positions, their gradients by
+backpropagation, AdamW steps over all tensors, and single tokens from the recurrent
+state, as large after a thousand positions as after one. The norms, the attention and
+the AdamW step are the library's (`layers`); the projections are plain matrix
+products of torch.
+
+As a program it trains on one batch of a workload, prints its curve, then continues
+the first sequences token by token from their prompts' states:
+    python -m paper_2505_17852_amd.recurrent --workload c5 --steps 200
+"""
+from __future__ import annotations
+
+import argparse
+import json
+import math
+import sys
+import time
+
+import torch
+
+from . import layers
+
+HEAD_DIM = 64  # of keys and values, or the hidden size where that is smaller
+
+
+class LinearLM:
+    """The model: one flat vector theta with its tensors as views, and the AdamW handle over them.
+
+    cfg: a workload's model configuration (n_layers, vocab, hidden, wdtype; the embedding has
+    the hidden size). kv_heads: key/value heads; query heads share them in equal groups."""
+
+    def __init__(self, cfg, seed: int = 0, lr: float = 1e-3, weight_decay: float = 0.1, state_bits: int = 32,
+                 kv_heads: int | None = None, device="cuda"):
+        self.V, self.H, self.L = int(cfg["vocab"]), int(cfg["hidden"]), int(cfg["n_layers"])
+        dtype = torch.bfloat16 if int(cfg["wdtype"]) else torch.float32
+        self.D = min(HEAD_DIM, self.H)
+        if self.H % self.D:
+            raise ValueError(f"hidden size {self.H} is no multiple of the head size {self.D}")
+        self.heads = self.H // self.D
+        self.kv = self.heads if kv_heads is None else kv_heads
+        H, width = self.H, (self.heads + 2 * self.kv) * self.D
+        shapes = {"emb": (self.V, H)}
+        for i in range(self.L):
+            shapes.update({f"norm_w{i}": (H,), f"norm_b{i}": (H,), f"qkv{i}": (width, H), f"out{i}": (H, H)})
+        shapes.update({"norm_w": (H,), "norm_b": (H,), "head": (self.V, H), "head_b": (self.V,)})
+        self.theta = torch.empty(sum(math.prod(s) for s in shapes.values()), dtype=dtype, device=device)
+        gen = torch.Generator(device=device)
+        gen.manual_seed(seed)
+        self.p, at = {}, 0
+        for name, shape in shapes.items():
+            n = math.prod(shape)
+            t = self.theta[at:at + n].view(shape)
+            at += n
+            if len(shape) == 2:
+                t.copy_(torch.randn(shape, generator=gen, device=device) / math.sqrt(H))
+            else:
+                t.fill_(1.0 if name.startswith("norm_w") else 0.0)
+            self.p[name] = t
+        # decays from 1 - 2^-3 to 1 - 2^-10 over the heads: memories of 8 to 1,000 positions
+        bits = torch.linspace(3.0, 10.0, self.kv, device=device) if self.kv > 1 else torch.full((1,), 6.0, device=device)
+        self.log_decay = torch.log1p(-torch.exp2(-bits))
+        self.opt = layers.AdamW(list(self.p.values()), lr=lr, state_bits=state_bits,
+                                weight_decay=[weight_decay if t.dim() == 2 else 0.0 for t in self.p.values()])
+
+    def _split(self, qkv):
+        """q, k and v as slices of the projection's output [..., (heads + 2 kv) D]."""
+        x = qkv.view(*qkv.shape[:-1], -1, self.D)
+        return x[..., :self.heads, :], x[..., self.heads:self.heads + self.kv, :], x[..., self.heads + self.kv:, :]
+
+    def forward(self, tokens: torch.Tensor, states=None, lengths: torch.Tensor | None = None, keep=None):
+        """Logits [B, T, V] and the layers' final states for tokens [B, T]; states: the initial ones (a
+        list of the layers', or None). keep: a list that receives what backward() needs."""
+        p, B, T = self.p, *tokens.shape
+        h = p["emb"][tokens.long()]
+        final = []
+        for i in range(self.L):
+            y, mean, rstd = layers.layer_norm(h, p[f"norm_w{i}"], p[f"norm_b{i}"])
+            qkv = torch.matmul(y, p[f"qkv{i}"].t())
+            o, s = layers.linear_attention(*self._split(qkv), self.log_decay, lengths=lengths, return_state=True,
+                                           initial_state=None if states is None else states[i])
+            final.append(s)
+            if keep is not None:
+                keep.append((h, y, mean, rstd, qkv, o))
+            h = h + torch.matmul(o.view(B, T, self.H), p[f"out{i}"].t())
+        y, mean, rstd = layers.layer_norm(h, p["norm_w"], p["norm_b"])
+        if keep is not None:
+            keep.append((h, y, mean, rstd))
+        return torch.matmul(y, p["head"].t()) + p["head_b"], final
+
+    def loss_and_gradients(self, tokens: torch.Tensor, mask: torch.Tensor | None):
+        """The masked mean cross-entropy of the next tokens (tokens [B, T + 1]), a device scalar, and the
+        gradients of all tensors, in their order."""
+        p, inputs, targets = self.p, tokens[:, :-1], tokens[:, 1:].long()
+        B, T = inputs.shape
+        keep = []
+        logits, _ = self.forward(inputs, keep=keep)
+        weight = torch.ones(B, T, device=tokens.device) if mask is None else mask.float()
+        weight = weight / weight.sum().clamp(min=1.0)
+        logp = torch.log_softmax(logits.float(), -1)
+        loss = -(logp.gather(2, targets.unsqueeze(2)).squeeze(2) * weight).sum()
+        dlogits = torch.exp(logp)
+        dlogits.scatter_add_(2, targets.unsqueeze(2), -torch.ones_like(targets, dtype=torch.float32).unsqueeze(2))
+        dlogits = (dlogits * weight.unsqueeze(2)).to(self.theta.dtype).view(B * T, self.V)
+        g = {}
+        h, y, mean, rstd = keep.pop()
+        g["head"] = torch.matmul(dlogits.t(), y.view(B * T, self.H))
+        g["head_b"] = dlogits.float().sum(0)
+        dh, g["norm_w"], g["norm_b"] = layers.layer_norm_backward(
+            torch.matmul(dlogits, p["head"]).view(B, T, self.H), h, p["norm_w"], mean, rstd)
+        for i in reversed(range(self.L)):
+            h, y, mean, rstd, qkv, o = keep.pop()
+            flat = dh.view(B * T, self.H)
+            g[f"out{i}"] = torch.matmul(flat.t(), o.view(B * T, self.H))
+            do = torch.matmul(flat, p[f"out{i}"]).view(o.shape)
+            dqkv = torch.empty_like(qkv)
+            dq, dk, dv = self._split(dqkv)
+            layers.linear_attention_backward(do, *self._split(qkv), self.log_decay, dq=dq, dk=dk, dv=dv)
+            flat = dqkv.view(B * T, -1)
+            g[f"qkv{i}"] = torch.matmul(flat.t(), y.view(B * T, self.H))
+            dx, g[f"norm_w{i}"], g[f"norm_b{i}"] = layers.layer_norm_backward(
+                torch.matmul(flat, p[f"qkv{i}"]).view(B, T, self.H), h, p[f"norm_w{i}"], mean, rstd)
+            dh = dh + dx
+        emb = torch.zeros(self.V, self.H, device=dh.device)
+        g["emb"] = emb.index_add_(0, inputs.reshape(-1).long(), dh.reshape(B * T, self.H).float())
+        return loss, [g[name] for name in p]
+
+    def train_step(self, tokens: torch.Tensor, mask: torch.Tensor | None, clip: float = 1.0) -> torch.Tensor:
+        """One AdamW step with the gradient clipped to a norm of `clip`; returns the loss before it. A
+        gradient that is not finite leaves parameters and moments as they are."""
+        loss, grads = self.loss_and_gradients(tokens, mask)
+        norm = torch.stack([torch.linalg.vector_norm(x.float()) for x in grads]).norm().view(1)
+        # 0 / norm is NaN where the norm is not finite: the step is then skipped
+        self.opt.step(grads, grad_scale=torch.clamp(clip / norm, max=1.0) + 0.0 * norm)
+        return loss
+
+    def step(self, tokens: torch.Tensor, states, slots: torch.Tensor | None = None) -> torch.Tensor:
+        """Logits [B, V] after one token for each sequence; the layers' states are updated in place."""
+        p, B = self.p, tokens.shape[0]
+        h = p["emb"][tokens.long()]
+        for i in range(self.L):
+            y, _, _ = layers.layer_norm(h, p[f"norm_w{i}"], p[f"norm_b{i}"])
+            q, k, v = self._split(torch.matmul(y, p[f"qkv{i}"].t()))
+            o = layers.linear_attention_step(q, k, v, self.log_decay, states[i], slots=slots)
+            h = h + torch.matmul(o.view(B, self.H), p[f"out{i}"].t())
+        y, _, _ = layers.layer_norm(h, p["norm_w"], p["norm_b"])
+        return torch.matmul(y, p["head"].t()) + p["head_b"]
+
+
+def answer(model: LinearLM, prompts: torch.Tensor, lengths: torch.Tensor | None, count: int) -> torch.Tensor:
+    """`count` tokens after each prompt [B, T] (of its own length), the likeliest one each: [B, count]."""
+    logits, states = model.forward(prompts, lengths=lengths)
+    B, T = prompts.shape
+    last = torch.full((B,), T, device=prompts.device) if lengths is None else lengths.long()
+    token = logits[torch.arange(B, device=prompts.device), last - 1].argmax(-1)
+    out = [token]
+    for _ in range(count - 1):
+        token = model.step(token, states).argmax(-1)
+        out.append(token)
+    return torch.stack(out, 1)
+
+
+def main(argv=None):
+    from . import workloads as wl
+    ap = argparse.ArgumentParser(description="trains a linear-attention language model on a batch of a workload")
+    ap.add_argument("--workload", default="c5", choices=sorted(wl.CONFIGS))
+    ap.add_argument("--steps", type=int, default=200)
+    ap.add_argument("--lr", type=float, default=3e-3)
+    ap.add_argument("--state-bits", type=int, default=32, choices=(32, 8))
+    ap.add_argument("--print-every", type=int, default=50)
+    args = ap.parse_args(argv)
+    dev = torch.device("cuda:0")
+    tokens, mask = wl.batch(args.workload)
+    tokens = torch.from_numpy(tokens).to(dev)
+    mask = None if mask is None else torch.from_numpy(mask).to(dev)
+    model = LinearLM(wl.model_cfg(args.workload), lr=args.lr, state_bits=args.state_bits, device=dev)
+    t0 = time.time()
+    for k in range(args.steps + 1):
+        loss = model.train_step(tokens, mask)
+        if k % args.print_every == 0 or k == args.steps:
+            print(json.dumps({"workload": args.workload, "step": k, "loss": round(float(loss), 5),
+                              "seconds": round(time.time() - t0, 2)}), flush=True)
+    half = tokens.shape[1] // 2
+    count = min(16, tokens.shape[1] - half)
+    got = answer(model, tokens[:4, :half], None, count)
+    print(json.dumps({"continued": got.tolist(), "batch": tokens[:4, half:half + count].tolist()}), flush=True)
+    return 0
+
+
+if __name__ == "__main__":
+    sys.exit(main())
