@@ -50,7 +50,7 @@ extern "C" {
 
 typedef struct {
     int32_t batch;      /* sequences, >= 0 */
-    int32_t length;     /* positions, >= 0 (the step: ignored) */
+    int32_t length;     /* positions, 0 .. 2^30 (the step: ignored) */
     int32_t q_heads;    /* a multiple of kv_heads */
     int32_t kv_heads;   /* > 0 */
     int32_t key_dim;    /* 1 .. ZO_LINATTN_MAX_DIM */
@@ -79,8 +79,8 @@ size_t zo_linear_attention_workspace_bytes(const zo_linattn* shape, int32_t back
  *   lengths        device int32 [B], or NULL (all T); values outside [0, T]
  *                  count as the nearer end
  *   initial_state  device fp32 [B][kv_heads][key_dim][value_dim], or NULL (zeros)
- *   final_state    the same shape, or NULL (not wanted); may be initial_state
- *                  itself (the states are then advanced in place)
+ *   final_state    the same shape, or NULL (not wanted); not initial_state itself
+ *                  (ZO_EINVAL): workgroups read the one while others write the other
  *   workspace, ws_bytes  at least zo_linear_attention_workspace_bytes(); NULL if that is 0 */
 int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_heads* k, const zo_heads* v,
                         const zo_heads* o, const float* log_decay, const int32_t* lengths,
@@ -94,7 +94,7 @@ int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_hea
  * (length 0: dinitial = dfinal).
  *   dout           gradient of o
  *   dfinal_state   device fp32, the final state's gradient, or NULL (zeros)
- *   dinitial_state device fp32, or NULL (not wanted); may be dfinal_state itself
+ *   dinitial_state device fp32, or NULL (not wanted); not dfinal_state itself (ZO_EINVAL)
  * Gradients from length_b on are zero. */
 int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, const zo_heads* q,
                                  const zo_heads* k, const zo_heads* v, const zo_heads* dq, const zo_heads* dk,

@@ -24,6 +24,7 @@ bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 int check_linattn(const zo_linattn* s) {
   if (!s) return fail(ZO_EINVAL, "shape is NULL");
   if (s->batch < 0 || s->length < 0) return fail(ZO_EINVAL, "batch and length must be >= 0");
+  if (s->length > 1 << 30) return fail(ZO_ESHAPE, "length must be <= 2^30");
   if (s->q_heads < 1 || s->kv_heads < 1 || s->q_heads % s->kv_heads)
     return fail(ZO_EINVAL, "q_heads (%d) must be a positive multiple of kv_heads (%d)", s->q_heads, s->kv_heads);
   if (s->key_dim < 1 || s->value_dim < 1) return fail(ZO_EINVAL, "key_dim and value_dim must be >= 1");
@@ -88,6 +89,8 @@ int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_hea
     return st;
   if (!log_decay) return fail(ZO_EINVAL, "log_decay is NULL");
   if (((uintptr_t)lengths & 3u) != 0) return fail(ZO_EINVAL, "lengths is not aligned to its type");
+  if (final_state && final_state == initial_state)
+    return fail(ZO_EINVAL, "final_state and initial_state must be different buffers");
   zo::LinCall c{};
   zo::LinPass& p = c.pass[0];
   p.x = heads(q);
@@ -137,6 +140,8 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
     return st;
   if (!log_decay) return fail(ZO_EINVAL, "log_decay is NULL");
   if (((uintptr_t)lengths & 3u) != 0) return fail(ZO_EINVAL, "lengths is not aligned to its type");
+  if (dinitial_state && dinitial_state == dfinal_state)
+    return fail(ZO_EINVAL, "dinitial_state and dfinal_state must be different buffers");
   const int share = s.q_heads / s.kv_heads;
   zo::LinCall c{};
   // dq: forward in time, the transposed state

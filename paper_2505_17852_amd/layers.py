@@ -184,14 +184,19 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     q [B, T, Hq, Dk], k [B, T, Hkv, Dk], v [B, T, Hkv, Dv] fp32 or bf16, any strides with
     contiguous heads; log_decay fp32 [Hkv]; scale defaults to Dk ** -0.5; states fp32
     [B, Hkv, Dk, Dv]; lengths int32 [B] or None (all T). The final state is returned with
-    return_state, or written into final_state (which may be initial_state)."""
+    return_state, or written into final_state (if that is initial_state, its values are copied first)."""
     L = lib()
     B, T, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 4, scale)
     states = (B, Hkv, Dk, Dv)
     o, ho = _new_heads(q, B, T, Hq, Dv) if out is None else (out, _heads(out, "out", (B, T, Hq, Dv), q))
     f32 = torch.float32
-    if final_state is None and return_state:
-        final_state = torch.empty(states, dtype=f32, device=q.device)
+    if final_state is None:
+        if return_state:
+            final_state = torch.empty(states, dtype=f32, device=q.device)
+    elif initial_state is not None and final_state.data_ptr() == initial_state.data_ptr():
+        # the kernels read the one while they write the other
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(q.device)):
+            initial_state = initial_state.clone()
     ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(s, 0), q)
     _check(L.zo_linear_attention(
         s, hq, hk, hv, ho, _flat(log_decay, "log_decay", f32, (Hkv,), q),

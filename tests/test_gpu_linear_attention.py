@@ -112,6 +112,50 @@ def test_forward_and_backward(layers, name, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Dk,Dv,T,state,ragged", [(64, 64, 70, True, True), (40, 24, 65, False, False),
+                                                  (128, 128, 130, True, True), (96, 128, 64, False, False),
+                                                  (64, 104, 33, True, False), (33, 64, 40, True, False), (8, 8, 1, True, False)])
+def test_many_states(layers, dtype, Dk, Dv, T, state, ragged):
+    """Enough states to fill the chip, heads that share none: the gradients of k and v from one walk."""
+    B, H = 16, 17
+    lengths = [0, 1, T] + [T - 3 * b for b in range(B - 3)] if ragged else None
+    s = make(np.random.default_rng(Dk + T), dtype, B, T, H, H, Dk, Dv, state, lengths)
+    check_forward(layers, s)
+    check_backward(layers, s)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_bad_value_among_many_states(layers, dtype, D):
+    """Values that are not finite in q, k, v or do of some heads: gradients of the others, and those of
+    positions that they do not reach, keep their bits."""
+    B, T, H = 16, 130, 17
+    s = make(np.random.default_rng(D), dtype, B, T, H, H, D, D, False)
+    args = dict(scale=s["scale"])
+    base = layers.linear_attention_backward(s["do_d"], s["q_d"], s["k_d"], s["v_d"], s["decay_d"], **args)
+    at = 70
+    # what a bad value at a position reaches: dq from it on (k, v) or there alone (do), dk and dv up to it (q, do)
+    # or there alone (k, v); and q no dq, k no dk, v no dv at all
+    before, after, there, none = slice(0, at), slice(at + 1, T), slice(at, at + 1), slice(0, 0)
+    kept = {"q": (none, after, after), "do": (None, after, after), "k": (before, none, None), "v": (before, None, none)}
+    for name in ("q", "do", "k", "v"):
+        for bad in (float("nan"), float("inf")):
+            x = {n: s[n + "_d"].clone() for n in ("do", "q", "k", "v")}
+            x[name][3, at, 5, 7] = bad
+            got = layers.linear_attention_backward(x["do"], x["q"], x["k"], x["v"], s["decay_d"], **args)
+            for g, w, part in zip(got, base, kept[name]):
+                others = torch.ones(B, H, dtype=torch.bool, device="cuda")
+                others[3, 5] = False
+                assert torch.equal(g.transpose(1, 2)[others], w.transpose(1, 2)[others]), name
+                if part is None:  # that position alone
+                    assert torch.equal(g[3, before, 5], w[3, before, 5]) and torch.equal(g[3, after, 5], w[3, after, 5]), name
+                    assert not torch.isfinite(g[3, there, 5]).all()
+                elif part is not none:
+                    assert torch.equal(g[3, part, 5], w[3, part, 5]), name
+                    assert not torch.isfinite(g[3, there, 5]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_decays_at_their_ends(layers, dtype):
     """No decay, total decay (log 0), and one that underflows within a chunk."""
     decay = np.array([0.0, -np.inf, -3.0, -40.0], dtype=np.float32)
@@ -235,6 +279,19 @@ def test_a_prompt_in_parts_is_the_prompt(layers, dtype):
     n = ref.attention_terms(T, D, D)
     close("o", torch.cat(parts, 1), want, ref.attention_bound(want, mag, dtype, n))
     close("state", state, wfinal, ref.state_bound(fmag, dtype, n))
+
+
+@pytest.mark.parametrize("shape", [(1, 2500, 8, 2, 64), (3, 500, 8, 1, 128), (1, 1400, 1, 1, 200)])
+def test_states_advanced_in_place(layers, shape):
+    """The final state into the initial one's buffer, with query heads and segments that read it too."""
+    B, T, Hq, Hkv, D = shape
+    s = make(np.random.default_rng(T), "bf16", B, T, Hq, Hkv, D, D, True)
+    want = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], initial_state=s["initial_d"],
+                                   return_state=True)
+    state = s["initial_d"].clone()
+    o, final = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], initial_state=state,
+                                       final_state=state)
+    assert final is state and torch.equal(o, want[0]) and torch.equal(state, want[1])
 
 
 STEPS = {

@@ -70,6 +70,7 @@ def error():
     (dict(value_dim=257), -2, "value_dim"), (dict(key_dim=1000), -2, "key_dim"), (dict(dtype=2), -1, "dtype"),
     (dict(scale=float("nan")), -1, "scale"), (dict(scale=float("inf")), -1, "scale"),
     (dict(batch=1 << 20, q_heads=1 << 14), -2, "batch"),
+    (dict(length=(1 << 30) + 1), -2, "length"),
 ])
 def test_linear_attention_shapes_are_refused(layers, bad, status, word):
     L, h = layers.lib(), heads(layers)
@@ -89,6 +90,11 @@ def test_linear_attention_pointers_are_refused(layers):
     for name in ("decay", "lengths", "initial", "final"):
         assert attention(layers, s, **{name: FAKE + 2}) == -1 and "aligned" in error()
     assert attention(layers, s, ws=FAKE + 8) == -1 and "workspace" in error()
+    assert attention(layers, s, initial=FAKE, final=FAKE) == -1 and "different" in error()
+    assert L.zo_linear_attention_backward(s, h, h, h, h, h, h, h, FAKE, None, None, FAKE, FAKE, FAKE, 1 << 40,
+                                          None) == -1 and "different" in error()
+    far = layers._HEADS.pack(FAKE, 1, (1 << 24) + 1, 1)
+    assert L.zo_linear_attention(s, h, far, h, h, FAKE, None, None, None, FAKE, 1 << 40, None) == -2
     assert L.zo_linear_attention(s, None, h, h, h, FAKE, None, None, None, FAKE, 1 << 40, None) == -1
     assert L.zo_linear_attention(None, h, h, h, h, FAKE, None, None, None, FAKE, 1 << 40, None) == -1
     assert L.zo_linear_attention_backward(s, h, h, h, None, h, h, h, FAKE, None, None, None, None, FAKE,
