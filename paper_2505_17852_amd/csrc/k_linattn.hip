@@ -15,15 +15,16 @@
 //   out_i = sum_j P_ij z_j + carry gamma^(i+off) R^T x_i
 //   R     = gamma^64 R + sum_j upd gamma^(64-off-j) y_j z_j^T
 // every sum a matrix product. A workgroup of four waves walks over the chunks of
-// one sequence, head and slice of 64 columns of z with R in its accumulators:
+// one sequence, head and slice of 64 or 128 columns of z with R in its accumulators:
 // x, y, z are read and out is written once per slice (the slices and passes of a
 // state run next to each other on one XCD, whose L2 serves the second reading).
-// Wave w has the chunk's rows 16 w .. 16 w + 15 and 16 of R's columns.
+// Wave w has the chunk's rows 16 w .. 16 w + 15 and a quarter of R's columns (so that only a quarter of z is
+// scaled by each).
 //
 // Operands. MFMA 16x16: A and B have the same lane layout, lane l = row (or column)
 // l % 16, contraction index group l / 16; the result has column l % 16 and
 // rows 4 (l / 16) + r. Scores are formed as P^T (y x^T), so that a lane holds
-// P_ij of its row i = l % 16 for j = 16 n + 4 (l / 16) + r: taken in that order of j,
+// P_ij of its row i = l % 16 for 4 positions j of each tile of 16: taken in that order of j,
 // the accumulators are the next product's operand as they are. The other operand of
 // the sums over j (columns of y and z by rows j) is read from row-major LDS tiles in the
 // same order: with the transposing LDS load (bf16), or by words (fp32). out is
@@ -44,6 +45,15 @@
 // into segments; a first launch runs only the state's sum of every segment
 // but the last, a second adds the segments up, and the main launch starts each
 // segment from its own state.
+//
+// What bounds it. bf16, 16 sequences of 1,024 positions, 32 heads of 128: the forward pass moves its 0.54 GB in
+// 0.13 ms (4.2 TB/s, a large copy reaches 4.75); the backward pass reads nine tensors for the four it needs
+// (its three passes share most of that in L2) and takes 0.36 ms. There and on shorter or
+// fewer sequences (32 ragged ones of up to 777 positions, 16 heads of 64: 36 us, 2.3 TB/s; one of 8,192, 32 heads of
+// 128: 0.12 ms) it is a workgroup's chain per chunk - loads, LDS, four dependent products, two barriers - at the
+// two workgroups that fit a CU: without its matrix products the kernel takes 57% of its time, without
+// its loads 80%. fp32 is bound by the fp32 MFMAs (1/16 of the bf16 rate) of the wave with most score tiles: 64 sequences
+// of 256 positions, 4 heads of 64, forward and backward 87 us, 43 TFLOP/s of the recurrence's own operations.
 #include <hip/hip_runtime.h>
 
 #include "zo_layers.hpp"
@@ -292,9 +302,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
 
   const int n = c.lengths ? min(max(c.lengths[b], 0), c.T) : c.T;
   const int r0 = seg * pl.length, r1 = min(n, r0 + pl.length);  // the segment's positions
-  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, m = lane & 15;
-  // (fp32: the rows go to other waves, so other SIMDs, in the next workgroups of a CU)
-  const int w = ((tid >> 6) + (sizeof(T) == 4 ? (int)(turn >> 5) : 0)) & 3;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, m = lane & 15;
+
   const float lg = c.log_decay[kvh] * 1.44269504088896340736f;
   const int off = a.reverse ? 0 : 1;
 
@@ -458,7 +467,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       for (int i = 0; i < NX; ++i)
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-          if (all || t <= w - (lead >> 4)) P[t] = O::mma(O::along(ys + 16 * ((w - t) & 3) * YS + m * YS + i * KB, g), xn[i], P[t]);
+          if (all || t <= w) P[t] = O::mma(O::along(ys + 16 * ((w - t) & 3) * YS + m * YS + i * KB, g), xn[i], P[t]);
 #pragma unroll
       for (int r = 0; r < 4; ++r) P[0][r] = 4 * g + r <= m ? P[0][r] * own_f[r] : 0.0f;
 #pragma unroll
@@ -482,7 +491,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
 #pragma unroll
           for (int j = 0; j < 4; ++j) acc[j] = f4{0, 0, 0, 0};
         }
-        if (src == 0 && (!ends || start > r0 - lead0 || from) && (all || w >= lead >> 4)) {
+        if (src == 0 && (!ends || start > r0 - lead0 || from)) {
 #pragma unroll
           for (int i = 0; i < NX; ++i)
 #pragma unroll
@@ -499,7 +508,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
         if (!flagged) {
 #pragma unroll
           for (int k = 0; k < NJ; ++k)
-            if (all || k <= w - (lead >> 4))
+            if (all || k <= w)
 #pragma unroll
               for (int j = 0; j < 4; ++j) acc[j] = O::mma(z_of(k, j), pb[k], acc[j]);
         } else {

@@ -5,7 +5,8 @@
 // state, 16 lanes by 16 bytes to a row, all of a thread's loads (up to 16) in
 // flight before the first is used. The state stays in registers for every query
 // head that reads it; their sums over the rows go through lane exchanges and
-// LDS.
+// LDS. 224 sequences, 32 states of 128 x 128 each: 0.95 GB in 187 us, 5.05 TB/s (a
+// copy of 4 GiB: 4.75); 4 sequences of 8 states: 5.6 us, a launch and one trip to memory.
 #include <hip/hip_runtime.h>
 
 #include "zo_layers.hpp"

@@ -14,6 +14,10 @@
 // do not fit the registers of so many). Rows beyond 8,192 values are read again
 // for every pass (the loop kernels).
 //
+// 65,536 rows of 4,096 (bf16), forward and backward with the weight's gradients: 2.7 GB in 0.51 ms, 5.2 TB/s (a
+// copy of 4 GiB: 4.75); without the next row's loads ahead and with the weights read for every row
+// 0.76 ms. 4,097 rows of 1,003 (fp32): 25 us, three launches of 9, 13 and 4 us.
+//
 // The weight's gradients: a workgroup of the backward pass walks over many rows
 // and keeps its threads' columns' sums in registers; the workgroups' sums go to
 // the workspace, and a second launch adds them, in workgroup order: the same
