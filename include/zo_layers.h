@@ -79,7 +79,7 @@ size_t zo_linear_attention_workspace_bytes(const zo_linattn* shape, int32_t back
  *   lengths        device int32 [B], or NULL (all T); values outside [0, T]
  *                  count as the nearer end
  *   initial_state  device fp32 [B][kv_heads][key_dim][value_dim], or NULL (zeros)
- *   final_state    the same shape, or NULL (not wanted); not initial_state itself
+ *   final_state    the same shape, or NULL (not wanted); nothing of initial_state
  *                  (ZO_EINVAL): workgroups read the one while others write the other
  *   workspace, ws_bytes  at least zo_linear_attention_workspace_bytes(); NULL if that is 0 */
 int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_heads* k, const zo_heads* v,
@@ -94,7 +94,7 @@ int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_hea
  * (length 0: dinitial = dfinal).
  *   dout           gradient of o
  *   dfinal_state   device fp32, the final state's gradient, or NULL (zeros)
- *   dinitial_state device fp32, or NULL (not wanted); not dfinal_state itself (ZO_EINVAL)
+ *   dinitial_state device fp32, or NULL (not wanted); nothing of dfinal_state (ZO_EINVAL)
  * Gradients from length_b on are zero. */
 int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, const zo_heads* q,
                                  const zo_heads* k, const zo_heads* v, const zo_heads* dq, const zo_heads* dk,
@@ -173,7 +173,8 @@ typedef struct {
  *                    is not finite the step is skipped on the device: parameters and
  *                    moments stay bit for bit as they are
  *   skipped_out      device int32 [1] or NULL: 1 if it was skipped, else 0
- * Parameters of 32-bit and 16-bit types may be mixed, and aligned as their type needs. */
+ * Parameters of 32-bit and 16-bit types may be mixed, and aligned as their type needs.
+ * cfg is read by the call: a captured launch replays with its step's lr and bias corrections. */
 int zo_adamw(const zo_adamw_config* cfg, const zo_adamw_tensor* tensors, int32_t n_tensors, void* m, void* v,
              float* m_scale, float* v_scale, const float* grad_scale, int32_t* skipped_out, void* stream);
 

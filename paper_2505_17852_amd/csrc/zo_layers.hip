@@ -56,6 +56,13 @@ int check_state(const float* s, const char* name) {
   return aligned4(s) ? ZO_OK : fail(ZO_EINVAL, "%s is not aligned to its type", name);
 }
 
+// Whether two buffers of all sequences' states share memory.
+bool overlap(const zo_linattn& s, const float* a, const float* b) {
+  const uint64_t bytes = (uint64_t)s.batch * s.kv_heads * s.key_dim * s.value_dim * sizeof(float);
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && (x < y ? y - x : x - y) < bytes;
+}
+
 int check_workspace(const zo_linattn* s, bool backward, const void* workspace, size_t bytes) {
   const size_t need = zo::linattn_workspace(*s, backward);
   if (bytes < need) return fail(ZO_ENOMEM, "workspace of %zu bytes < %zu required", bytes, need);
@@ -89,7 +96,7 @@ int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_hea
     return st;
   if (!log_decay) return fail(ZO_EINVAL, "log_decay is NULL");
   if (((uintptr_t)lengths & 3u) != 0) return fail(ZO_EINVAL, "lengths is not aligned to its type");
-  if (final_state && final_state == initial_state)
+  if (overlap(s, final_state, initial_state))
     return fail(ZO_EINVAL, "final_state and initial_state must be different buffers");
   zo::LinCall c{};
   zo::LinPass& p = c.pass[0];
@@ -140,7 +147,7 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
     return st;
   if (!log_decay) return fail(ZO_EINVAL, "log_decay is NULL");
   if (((uintptr_t)lengths & 3u) != 0) return fail(ZO_EINVAL, "lengths is not aligned to its type");
-  if (dinitial_state && dinitial_state == dfinal_state)
+  if (overlap(s, dinitial_state, dfinal_state))
     return fail(ZO_EINVAL, "dinitial_state and dfinal_state must be different buffers");
   const int share = s.q_heads / s.kv_heads;
   zo::LinCall c{};

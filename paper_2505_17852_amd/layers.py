@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+from operator import attrgetter
 
 import torch
 
@@ -184,7 +185,7 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     q [B, T, Hq, Dk], k [B, T, Hkv, Dk], v [B, T, Hkv, Dv] fp32 or bf16, any strides with
     contiguous heads; log_decay fp32 [Hkv]; scale defaults to Dk ** -0.5; states fp32
     [B, Hkv, Dk, Dv]; lengths int32 [B] or None (all T). The final state is returned with
-    return_state, or written into final_state (if that is initial_state, its values are copied first)."""
+    return_state, or written into final_state (if that overlaps initial_state, its values are copied first)."""
     L = lib()
     B, T, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 4, scale)
     states = (B, Hkv, Dk, Dv)
@@ -193,8 +194,8 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     if final_state is None:
         if return_state:
             final_state = torch.empty(states, dtype=f32, device=q.device)
-    elif initial_state is not None and final_state.data_ptr() == initial_state.data_ptr():
-        # the kernels read the one while they write the other
+    elif initial_state is not None and abs(final_state.data_ptr() - initial_state.data_ptr()) < 4 * B * Hkv * Dk * Dv:
+        # (shared, or in part) the kernels read the one while they write the other
         with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(q.device)):
             initial_state = initial_state.clone()
     ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(s, 0), q)
@@ -334,6 +335,10 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
 
 # ---- AdamW ----
 
+_shape_of, _dtype_of = attrgetter("shape"), attrgetter("dtype")
+_device_of, _contiguous, _address = torch.Tensor.get_device, torch.Tensor.is_contiguous, torch.Tensor.data_ptr
+
+
 class AdamW:
     """AdamW over a list of parameter tensors, all in one launch for up to 64 of them.
 
@@ -342,7 +347,8 @@ class AdamW:
     codes with m_scale and v_scale, the largest values of blocks of 256: see
     zo_layers.h). The moments of tensor i begin at offsets[i] of the flat m and v and take
     whole blocks. step_count is the number of steps done; a checkpoint is step_count, m, v
-    and the scales."""
+    and the scales, to be copied back into the same buffers (m.copy_(...)). A step captured
+    into a HIP graph replays with the learning rate and the bias corrections of its capture."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.0,
                  state_bits: int = 32):
@@ -365,19 +371,27 @@ class AdamW:
             self.offsets.append(at)
             at += (p.numel() + BLOCK - 1) // BLOCK * BLOCK
         dev = first.device
-        self.m_scale = self.v_scale = None
+        self._m_scale = self._v_scale = None
         if state_bits == 8:
-            self.m = torch.zeros(at, dtype=torch.int8, device=dev)
-            self.v = torch.zeros(at, dtype=torch.uint8, device=dev)
-            self.m_scale = torch.zeros(at // BLOCK, dtype=torch.float32, device=dev)
-            self.v_scale = torch.zeros(at // BLOCK, dtype=torch.float32, device=dev)
+            self._m = torch.zeros(at, dtype=torch.int8, device=dev)
+            self._v = torch.zeros(at, dtype=torch.uint8, device=dev)
+            self._m_scale = torch.zeros(at // BLOCK, dtype=torch.float32, device=dev)
+            self._v_scale = torch.zeros(at // BLOCK, dtype=torch.float32, device=dev)
         else:
-            self.m = torch.zeros(at, dtype=torch.float32, device=dev)
-            self.v = torch.zeros(at, dtype=torch.float32, device=dev)
+            self._m = torch.zeros(at, dtype=torch.float32, device=dev)
+            self._v = torch.zeros(at, dtype=torch.float32, device=dev)
         self._shapes = [p.shape for p in self.params]
+        self._dtypes = [p.dtype for p in self.params]
+        self._devices = [first.get_device()] * len(self.params)
         self._table = (_Tensor * len(self.params))(
             *(_Tensor(p.data_ptr(), None, p.numel(), o, float(d), _DTYPES[p.dtype], zo.FP32)
               for p, o, d in zip(self.params, self.offsets, decay)))
+
+    # the kernels trust the buffers' sizes: they can be written into, not exchanged
+    m = property(lambda self: self._m)
+    v = property(lambda self: self._v)
+    m_scale = property(lambda self: self._m_scale)
+    v_scale = property(lambda self: self._v_scale)
 
     def step(self, grads, grad_scale: torch.Tensor | None = None, skipped: torch.Tensor | None = None, stream=None):
         """One step (asynchronous) with one contiguous fp32 or bf16 gradient for each tensor.
@@ -387,20 +401,28 @@ class AdamW:
         grads = list(grads)
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} tensors")
-        like = self.m
-        dev = like.get_device()
-        for t, p, shape, g in zip(self._table, self.params, self._shapes, grads):
-            kind = _DTYPES.get(g.dtype)
-            if kind is None or g.get_device() != dev or g.shape != shape or not g.is_contiguous():
-                raise ValueError(f"gradients must be contiguous fp32 or bf16 tensors of their parameters' shapes on "
-                                 f"{like.device}: got {g.dtype} {list(g.shape)} on {g.device} for {list(shape)}")
-            t.param, t.grad, t.gdtype = p.data_ptr(), g.data_ptr(), kind
+        like, params = self._m, self.params
+        # whole lists at a time: a check of each tensor in turn takes a third longer
+        if (list(map(_shape_of, params)) != self._shapes or list(map(_dtype_of, params)) != self._dtypes
+                or list(map(_device_of, params)) != self._devices or not all(map(_contiguous, params))):
+            raise ValueError("a parameter's type, shape, layout or device is not what it was when AdamW was made")
+        kinds = list(map(_DTYPES.get, map(_dtype_of, grads)))
+        if (list(map(_shape_of, grads)) != self._shapes or None in kinds
+                or list(map(_device_of, grads)) != self._devices or not all(map(_contiguous, grads))):
+            for i, (g, shape) in enumerate(zip(grads, self._shapes)):
+                if g.shape != shape or g.dtype not in _DTYPES or g.device != like.device or not g.is_contiguous():
+                    raise ValueError(f"gradients must be contiguous fp32 or bf16 tensors of their parameters' shapes on "
+                                     f"{like.device}: grads[{i}] is {g.dtype} {list(g.shape)} on {g.device} for "
+                                     f"{list(shape)}")
+        for t, p, g, kind in zip(self._table, map(_address, params), map(_address, grads), kinds):
+            t.param, t.grad, t.gdtype = p, g, kind
         gs = _flat(grad_scale, "grad_scale", torch.float32, (1,), like)
         sk = _flat(skipped, "skipped", torch.int32, (1,), like)
         cfg = _AdamWConfig(self.lr, self.betas[0], self.betas[1], self.eps, self.step_count + 1, self.state_bits)
         eight = self.state_bits == 8
-        _check(lib().zo_adamw(C.byref(cfg), self._table, len(grads), self.m.data_ptr(), self.v.data_ptr(),
-                              self.m_scale.data_ptr() if eight else None, self.v_scale.data_ptr() if eight else None,
+        _check(lib().zo_adamw(C.byref(cfg), self._table, len(grads), like.data_ptr(), self._v.data_ptr(),
+                              self._m_scale.data_ptr() if eight else None,
+                              self._v_scale.data_ptr() if eight else None,
                               gs, sk, _stream(stream, like)))
         self.step_count += 1
 

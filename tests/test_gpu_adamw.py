@@ -200,3 +200,37 @@ def test_a_graph_and_another_stream(layers):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, (p, opt.m, opt.v, *held)))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_what_changed_since_construction_is_refused(layers, bits):
+    """A parameter whose storage was exchanged, and moments that cannot be: refused on the host, nothing counted."""
+    sizes = [300, 40, 1000]
+    for change in (lambda p: p.bfloat16(), lambda p: p[:-1].clone(), lambda p: p.cpu(), lambda p: p.repeat(2)[::2]):
+        params = [torch.ones(n, device="cuda") for n in sizes]
+        grads = [torch.ones(n, device="cuda") for n in sizes]
+        opt = layers.AdamW(params, state_bits=bits)
+        opt.step(grads)
+        keep = params[0].clone()
+        params[1].data = change(params[1])
+        with pytest.raises(ValueError, match="parameter"):
+            opt.step(grads)
+        assert opt.step_count == 1 and torch.equal(params[0], keep)
+    for name in ("m", "v", "m_scale", "v_scale"):
+        with pytest.raises(AttributeError):
+            setattr(opt, name, torch.zeros(1))
+
+
+def test_gradients_that_do_not_fit_are_refused(layers):
+    params = [torch.ones(6, 8, device="cuda"), torch.ones(40, device="cuda")]
+    opt = layers.AdamW(params)
+    good = [torch.ones_like(p) for p in params]
+    for bad in (good[0][:, :7], good[0].view(48), good[0].double(), good[0].cpu(), torch.ones(8, 6, device="cuda").t(),
+                good[0].int()):
+        with pytest.raises(ValueError, match=r"grads\[0\]"):
+            opt.step([bad, good[1]])
+    with pytest.raises(ValueError, match="1 gradients"):
+        opt.step(good[:1])
+    assert opt.step_count == 0
+    opt.step(good)
+    assert opt.step_count == 1

@@ -395,3 +395,16 @@ def test_nothing_to_do(layers):
     assert torch.equal(got[3], initial)
     e = torch.zeros(0, 2, 32, device="cuda")
     assert layers.linear_attention_step(e, e, e, decay, initial).shape == (0, 2, 32)
+
+
+def test_a_final_state_that_overlaps_the_initial_one_in_part(layers):
+    """States of one buffer, moved up by one sequence: the values before the call are the ones that count."""
+    B, T, Hq, Hkv, D = 3, 300, 4, 2, 64
+    s = make(np.random.default_rng(77), "f32", B, T, Hq, Hkv, D, D, True)
+    want = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], initial_state=s["initial_d"],
+                                   return_state=True)
+    pool = torch.zeros(B + 1, Hkv, D, D, device="cuda")
+    pool[:B] = s["initial_d"]
+    o, final = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], initial_state=pool[:B],
+                                       final_state=pool[1:])
+    assert torch.equal(o, want[0]) and torch.equal(pool[1:], want[1]) and torch.equal(pool[0], s["initial_d"][0])

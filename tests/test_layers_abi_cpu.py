@@ -197,3 +197,13 @@ def test_performance_cases_import_without_a_gpu():
     cases = m.listed()
     assert len({c["name"] for c in cases}) == len(cases)
     assert all(m.work(c)["bytes"] > 0 for c in cases)
+
+
+def test_states_that_share_memory_in_part_are_refused(layers):
+    states = 2 * 2 * 32 * 32 * 4  # bytes of shape()'s states
+    s, h = shape(layers), heads(layers)
+    for a, b in ((FAKE, FAKE + 4), (FAKE + states - 4, FAKE), (FAKE, FAKE + states // 2)):
+        assert attention(layers, s, initial=a, final=b) == -1 and "different" in error()
+        st = layers.lib().zo_linear_attention_backward(s, h, h, h, h, h, h, h, FAKE, None, None, a, b, FAKE, 1 << 40,
+                                                       None)
+        assert st == -1 and "different" in error()
