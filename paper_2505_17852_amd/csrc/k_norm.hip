@@ -218,8 +218,15 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormAr
     rx.get(lane, D, x);
     rdy.get(lane, D, dy);
     const float rs = rstd;
+    // zero past the row's end too: a large mean times rstd may not be finite where no value is
 #pragma unroll
-    for (int i = 0; i < kVals; ++i) x[i] = (x[i] - mean) * rs;  // past the row's end dy is zero, and x never stored
+    for (int c = 0; c < kVals / VEC; ++c)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        float& v = x[c * VEC + e];
+        const int j = (c * TPR + lane) * VEC;
+        v = (even ? j : j + e) < D ? (v - mean) * rs : 0.0f;
+      }
     // the next row's loads before this one's sums (the last row has none: itself once more, in place or not)
     load(r + step < a.rows ? r + step : r);
     float s[2] = {0, 0};

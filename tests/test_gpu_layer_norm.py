@@ -186,3 +186,18 @@ def test_no_rows(layers):
     y, mean, rstd = layers.layer_norm(x)
     dx, dw, db = layers.layer_norm_backward(x, x, None, mean, rstd)
     assert y.shape == x.shape == dx.shape and not dw.any() and not db.any()
+
+
+@pytest.mark.parametrize("D", [100, 96, 250])
+def test_constant_rows_whose_mean_times_rstd_overflows(layers, D):
+    """Rows of 2^120 (sums and means are exact): xhat is zero, dx = rstd (dy - avg(dy)), though 2^120 rstd is not finite.
+    The average carries at most 38 roundings of sums and a division, dx four more."""
+    x = torch.full((5, D), 2.0 ** 120, device="cuda")
+    dy, dy_h = rand(np.random.default_rng(D), (5, D))
+    y, mean, rstd = layers.layer_norm(x, eps=EPS)
+    assert not y.any() and bool((mean == 2.0 ** 120).all())
+    dx, dw, db = layers.layer_norm_backward(dy, x, None, mean, rstd)
+    g, r = dy_h.astype(np.float64), 1.0 / np.sqrt(EPS)
+    want = r * (g - g.mean(1, keepdims=True))
+    close("dx", dx, want, 43 * ref.unit("f32") * r * (np.abs(g) + np.abs(g).mean(1, keepdims=True)))
+    assert not dw.any() and torch.isfinite(db).all()
