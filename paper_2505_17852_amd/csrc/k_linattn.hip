@@ -425,8 +425,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   if (a.dx < DX) Y::clear(ys);
   if (zd < SL) Z::clear(zs);
   __syncthreads();
-  static_assert(SL == 64 || SL == 128, "");
-  f4 acc[4];  // (with two parts of the output every step is a chunk of its own: one source)
+  static_assert(SL == 64 || SL == 128, "one part of the output, or two (and then one source: acc holds one part)");
+  f4 acc[4];
   int src = 0, turn_of = 0;
   for (int start = r0 - lead0; start < r1; turn_of ^= 1) {
     const int lead = max(r0 - start, 0);
@@ -506,8 +506,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
         }
         if (src == 0 && (!ends || start > r0 - lead0 || from)) {
 #pragma unroll
-          for (int i = 0; i < NX; ++i)
-{
+          for (int i = 0; i < NX; ++i) {
             const auto r_of = [&](int j) { return O::along(rs + (64 * part + 16 * j + m) * YS + i * KB, g); };
             O::mma({r_of(0), r_of(1), r_of(2), r_of(3)}, xn[i], acc);
           }
@@ -526,7 +525,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
         } else {
 #pragma unroll
           for (int k = 0; k < NJ; ++k)
-            O::mma({only_finite<T>(z_of(k, 0)), only_finite<T>(z_of(k, 1)), only_finite<T>(z_of(k, 2)), only_finite<T>(z_of(k, 3))},
+            O::mma({only_finite<T>(z_of(k, 0)), only_finite<T>(z_of(k, 1)), only_finite<T>(z_of(k, 2)),
+                    only_finite<T>(z_of(k, 3))},
                    pb[k], acc);
           // the products of z that are not finite, for the rows they reach
           constexpr int WORDS = 4 * NJ;
@@ -812,7 +812,10 @@ __global__ __launch_bounds__(kThreads) void linattn_scan_kernel(LinCall c, Plan 
   }
 }
 
-// Segments of a call: enough workgroups for two on every CU, none shorter than four chunks.
+// Segments of a call: enough workgroups for two on every CU, none shorter than four chunks; one where 256 workgroups
+// are there already (the states' pass over y and z costs more than the shorter chain saves: 512 workgroups, 32
+// sequences of 777, bf16, 16 heads on 4 states of 64: 39 us, in two segments 48; 16 sequences of 1,024, 32 heads of
+// 128: 137 and 176).
 void split(int64_t workgroups, int T, int* segments, int* length) {
   int64_t s = workgroups >= 256 || workgroups == 0 ? 1 : (512 + workgroups - 1) / workgroups;
   const int64_t most = T / (4 * kChunk);
