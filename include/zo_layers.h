@@ -40,8 +40,8 @@ extern "C" {
  * leaves every earlier output of its sequence as it would be without it.
  *
  * Precision: products and sums as fp32; with bf16 activations the operands
- * formed inside (the masked scores, and the states that queries read) are
- * rounded to bf16, states and their gradients are not. */
+ * formed inside (the masked scores, and the states that queries read) are held in
+ * two bf16 parts, 2^-16 of them left out at most, states and their gradients in fp32. */
 
 /* Head sizes up to ZO_LINATTN_MAX_DIM (ZO_ESHAPE beyond). */
 #define ZO_LINATTN_MAX_DIM 256

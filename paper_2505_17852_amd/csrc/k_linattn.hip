@@ -30,11 +30,15 @@
 // same order: with the transposing LDS load (bf16), or by words (fp32). out is
 // formed transposed too, so that a lane holds 4 neighbouring columns of one row.
 //
-// Precision: fp32 accumulators and state. bf16 rounds P, and R where x reads it, to
-// bf16 (the rounding of an input each); the state's own sum takes gamma^(..) z in
+// Precision: fp32 accumulators and state. With bf16 inputs P, and R where x reads it, meet
+// them as two bf16 parts each, which leave out 2^-16 at most: the outputs' error is that of their own
+// rounding (one part each adds another of that size: 1.4 times the error, for a tenth less time, a sixth where
+// slices have 128 columns). The state's own sum takes gamma^(..) z in
 // three bf16 parts, all of its fp32 value, since what is lost there would stay for all later
-// positions (two parts leave out 2^-17 and take 5% less time). fp32 runs on fp32 MFMAs
-// throughout.
+// positions. fp32 runs on fp32 MFMAs throughout.
+//
+// Slices of 128 columns: both parts of all of R would leave LDS for one workgroup per CU, so x
+// reads 64 columns at a time, with two barriers more.
 //
 // Positions past a sequence's length are never read. P of later positions is set
 // to zero, not multiplied by it; a z that is not finite would still turn those zeros
@@ -164,6 +168,16 @@ __device__ __forceinline__ typename Op<T>::Frag only_finite(typename Op<T>::Frag
   return __builtin_bit_cast(typename Op<T>::Frag, v);
 }
 
+// Four values as bf16, and what that leaves out of each.
+__device__ __forceinline__ uint2 halves(const f4& x, float* rest) {
+  const uint2 p{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
+  rest[0] = x[0] - __uint_as_float(p.x << 16);
+  rest[1] = x[1] - __uint_as_float(p.x & 0xffff0000u);
+  rest[2] = x[2] - __uint_as_float(p.y << 16);
+  rest[3] = x[3] - __uint_as_float(p.y & 0xffff0000u);
+  return p;
+}
+
 // A value that all lanes share, in a scalar register.
 __device__ __forceinline__ float scalar(float x) {
   return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(x)));
@@ -274,8 +288,10 @@ __device__ __forceinline__ void store_rows(const f4 (&acc)[4], T* row, bool exis
   }
 }
 
+// Waves per SIMD: bf16 states of 64 rows leave room for three (64 sequences of 1,024 positions, 16 heads of 64, backward:
+// 307 us, with two 320; of 60, whose loads take more registers, 417 and 414: two).
 template <typename T, int DX, int SL, bool even, bool state_only>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 2 : 1) void linattn_chunk_kernel(LinCall c, Plan pl) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX == 64 && even ? 3 : (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 2 : 1) void linattn_chunk_kernel(LinCall c, Plan pl) {
   typedef Op<T> O;
   typedef typename O::Frag Frag;
   typedef Staged<T, DX, even> Y;
@@ -283,10 +299,12 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   constexpr int EL = 16 / sizeof(T), KB = O::KB;
   constexpr int YS = Y::STRIDE, ZS = Z::STRIDE;
   constexpr int NX = DX / KB, NJ = kChunk / KB;        // operand sets along a row of x, over the chunk's positions
-  constexpr int MT = DX / 16, NW = SL / 64;           // tiles of 16: R's rows, a wave's of its columns
+  constexpr int MT = DX / 16, NW = SL / 64;           // tiles of 16: R's rows, a wave's of its columns (w, w + 4)
+  constexpr int FP = sizeof(T) == 2 ? 2 : 1;          // parts of P, and of R where x reads it
+  constexpr int RC = FP == 2 ? 64 : SL;               // columns of R that x reads at a time
   __shared__ __align__(16) T ys[kChunk * YS];
   __shared__ __align__(16) T zs[kChunk * ZS];
-  __shared__ __align__(16) T rs[state_only ? 1 : SL * YS];  // R^T where x reads it
+  __shared__ __align__(16) T rs[state_only ? 1 : FP * RC * YS];  // R^T where x reads it
   __shared__ int bad[2];
 
   // groups go round the XCDs (workgroup i runs on XCD i % 8), the members of one stay together
@@ -324,9 +342,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
     if (r0 >= n && seg > 0) return;
   }
 
-  // R: rows 16 i + 4 g + r, columns col + 16 (w NW + u) + m
+  // R: rows 16 i + 4 g + r, columns col + 64 u + 16 w + m
   f4 R[NW][MT];
-  const int rz = col + 16 * w * NW + m;
+  const int rz = col + 16 * w + m;
   const float* from = nullptr;
   {
     bool turned = false;
@@ -344,7 +362,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       const int sx = turned ? 1 : a.dz, sz = turned ? a.dx : 1;
 #pragma unroll
       for (int u = 0; u < NW; ++u) {
-        const int z = rz + 16 * u;
+        const int z = rz + 64 * u;
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -427,6 +445,17 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
   __syncthreads();
   static_assert(SL == 64 || SL == 128, "one part of the output, or two (and then one source: acc holds one part)");
   f4 acc[4];
+  // bf16: 64 columns of R as two parts, the second of what the first left out
+  const auto put_r = [&](int u) {
+    T* to = rs + (16 * w + m) * YS + 4 * g;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      float rest[4];
+      const uint2 high = halves(R[u][i], rest);
+      *(uint2*)(to + 16 * i) = high;
+      *(uint2*)(to + 64 * YS + 16 * i) = uint2{bf16_pair(rest[0], rest[1]), bf16_pair(rest[2], rest[3])};
+    }
+  };
   int src = 0, turn_of = 0;
   for (int start = r0 - lead0; start < r1; turn_of ^= 1) {
     const int lead = max(r0 - start, 0);
@@ -434,12 +463,17 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
     zn.put(zs, lead, zd);
     if constexpr (!state_only) {
       if (zn.any_not_finite()) bad[turn_of] = 1;
-      if (src == 0)
+      if (src == 0) {
+        if constexpr (FP == 2) {
+          put_r(0);
+        } else {
 #pragma unroll
-        for (int u = 0; u < NW; ++u)
+          for (int u = 0; u < NW; ++u)
 #pragma unroll
-          for (int i = 0; i < MT; ++i)
-            store_run<T, 4>(rs + (16 * (w * NW + u) + m) * YS + 16 * i + 4 * g, (const float*)&R[u][i]);
+            for (int i = 0; i < MT; ++i)
+              store_run<T, 4>(rs + (64 * u + 16 * w + m) * YS + 16 * i + 4 * g, (const float*)&R[u][i]);
+        }
+      }
     }
     __syncthreads();
     const bool flagged = !state_only && bad[turn_of];
@@ -487,29 +521,41 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       for (int t = 1; t < 4; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) P[t][r] = t <= w ? P[t][r] * far_f[r] * tile_f[t - 1] : 0.0f;
-      Frag pb[NJ];
+      Frag pb[FP][NJ];
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        if constexpr (sizeof(T) == 2)
-          pb[j] = __builtin_bit_cast(Frag, u4{bf16_pair(P[2 * j][0], P[2 * j][1]), bf16_pair(P[2 * j][2], P[2 * j][3]),
-                                              bf16_pair(P[2 * j + 1][0], P[2 * j + 1][1]),
-                                              bf16_pair(P[2 * j + 1][2], P[2 * j + 1][3])});
-        else
-          pb[j] = P[j];
+        if constexpr (FP == 2) {
+          float rest[8];
+          const uint2 a = halves(P[2 * j], rest), b = halves(P[2 * j + 1], rest + 4);
+          pb[0][j] = __builtin_bit_cast(Frag, u4{a.x, a.y, b.x, b.y});
+          pb[1][j] = __builtin_bit_cast(Frag, u4{bf16_pair(rest[0], rest[1]), bf16_pair(rest[2], rest[3]),
+                                                 bf16_pair(rest[4], rest[5]), bf16_pair(rest[6], rest[7])});
+        } else {
+          pb[0][j] = P[j];
+        }
       }
       // the output, 64 columns at a time
 #pragma unroll
       for (int part = 0; part < SL / 64; ++part) {
+        if (FP == 2 && part > 0) {  // (slices of 128 have one source)
+          __syncthreads();
+          put_r(part);
+          __syncthreads();
+        }
         if (src == 0) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) acc[j] = f4{0, 0, 0, 0};
         }
         if (src == 0 && (!ends || start > r0 - lead0 || from)) {
 #pragma unroll
-          for (int i = 0; i < NX; ++i) {
-            const auto r_of = [&](int j) { return O::along(rs + (64 * part + 16 * j + m) * YS + i * KB, g); };
-            O::mma({r_of(0), r_of(1), r_of(2), r_of(3)}, xn[i], acc);
-          }
+          for (int i = 0; i < NX; ++i)
+#pragma unroll
+            for (int q = 0; q < FP; ++q) {
+              const auto r_of = [&](int j) {
+                return O::along(rs + ((FP == 2 ? 64 * q : 64 * part) + 16 * j + m) * YS + i * KB, g);
+              };
+              O::mma({r_of(0), r_of(1), r_of(2), r_of(3)}, xn[i], acc);
+            }
 #pragma unroll
           for (int j = 0; j < 4; ++j) acc[j] *= xf;
         }
@@ -521,13 +567,19 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
         if (!flagged) {
 #pragma unroll
           for (int k = 0; k < NJ; ++k)
-            if (all || k < 2 || w >= 2) O::mma({z_of(k, 0), z_of(k, 1), z_of(k, 2), z_of(k, 3)}, pb[k], acc);
+            if (all || k < 2 || w >= 2) {
+              const Frag z[4] = {z_of(k, 0), z_of(k, 1), z_of(k, 2), z_of(k, 3)};
+#pragma unroll
+              for (int q = 0; q < FP; ++q) O::mma(z, pb[q][k], acc);
+            }
         } else {
 #pragma unroll
-          for (int k = 0; k < NJ; ++k)
-            O::mma({only_finite<T>(z_of(k, 0)), only_finite<T>(z_of(k, 1)), only_finite<T>(z_of(k, 2)),
-                    only_finite<T>(z_of(k, 3))},
-                   pb[k], acc);
+          for (int k = 0; k < NJ; ++k) {
+            const Frag z[4] = {only_finite<T>(z_of(k, 0)), only_finite<T>(z_of(k, 1)), only_finite<T>(z_of(k, 2)),
+                               only_finite<T>(z_of(k, 3))};
+#pragma unroll
+            for (int q = 0; q < FP; ++q) O::mma(z, pb[q][k], acc);
+          }
           // the products of z that are not finite, for the rows they reach
           constexpr int WORDS = 4 * NJ;
           int zat = 64 * part + 4 * g;
@@ -536,11 +588,15 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
           for (int at = 0; at < kChunk; ++at) {
             // P of position at: in lanes of group (at / 4) % 4, values 4 t + at % 4 of the operands
             const int t = w - (at >> 4), value = (t & 3) * 4 + (at & 3), want = sizeof(T) == 2 ? value >> 1 : value;
-            uint32_t word = 0;
+            float p = 0;
 #pragma unroll
-            for (int e = 0; e < WORDS; ++e) word = e == want ? __builtin_bit_cast(u4, pb[e >> 2])[e & 3] : word;
-            word = (uint32_t)__shfl((int)word, m + 16 * ((at >> 2) & 3), 64);
-            const float p = __uint_as_float(sizeof(T) == 4 ? word : at & 1 ? word & 0xffff0000u : word << 16);
+            for (int q = 0; q < FP; ++q) {
+              uint32_t word = 0;
+#pragma unroll
+              for (int e = 0; e < WORDS; ++e) word = e == want ? __builtin_bit_cast(u4, pb[q][e >> 2])[e & 3] : word;
+              word = (uint32_t)__shfl((int)word, m + 16 * ((at >> 2) & 3), 64);
+              p += __uint_as_float(sizeof(T) == 4 ? word : at & 1 ? word & 0xffff0000u : word << 16);
+            }
 #pragma unroll
             for (int d = 0; d < 16; ++d) {
               const float v = to_f32(zs[at * ZS + zat + 16 * (d >> 2) + (d & 3)]);
@@ -572,7 +628,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       Frag part[NW][PARTS];
 #pragma unroll
       for (int u = 0; u < NW; ++u) {
-        const T* zt = zs + k * KB * ZS + 16 * (w * NW + u);
+        const T* zt = zs + k * KB * ZS + 64 * u + 16 * w;
         const Frag own = O::down(zt, zt + 16 * ZS, ZS, g, m);
         if constexpr (sizeof(T) == 2) {
           const u4 raw = __builtin_bit_cast(u4, own);
@@ -642,7 +698,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 ? DX < 256 : DX < 128) ? 
       for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int x = 16 * i + 4 * g + r, z = rz + 16 * u;
+          const int x = 16 * i + 4 * g + r, z = rz + 64 * u;
           if (x < a.dx && z < a.dz) to[turned ? z * a.dx + x : x * a.dz + z] = R[u][i][r];
         }
 }

@@ -408,3 +408,41 @@ def test_a_final_state_that_overlaps_the_initial_one_in_part(layers):
     o, final = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], initial_state=pool[:B],
                                        final_state=pool[1:])
     assert torch.equal(o, want[0]) and torch.equal(pool[1:], want[1]) and torch.equal(pool[0], s["initial_d"][0])
+
+
+@pytest.mark.parametrize("name", ["odd_heads", "unequal", "shared", "wide", "widest", "wide_odd", "ragged", "long",
+                                  "long_ragged"])
+def test_bf16_results_as_near_as_fp32_operands_leave_them(layers, name):
+    """Scores and states meet the bf16 inputs as two bf16 parts each: what is left out of an operand is at most
+    unit(bf16) of its first part's own rounding, unit(bf16)^2 = 2^-16; the rest is fp32 sums and the output's rounding."""
+    B, T, Hq, Hkv, Dk, Dv, state, lengths = SHAPES[name]
+    s = make(np.random.default_rng(len(name) + 90), "bf16", B, T, Hq, Hkv, Dk, Dv, state, lengths)
+    _near_fp32(layers, s)
+
+
+@pytest.mark.parametrize("D,T", [(64, 130), (96, 70), (128, 200), (104, 65)])
+def test_bf16_results_of_many_states_as_near(layers, D, T):
+    """The same where there are states enough for the wider slices."""
+    _near_fp32(layers, make(np.random.default_rng(D), "bf16", 16, T, 17, 17, D, D, True))
+
+
+def _near_fp32(layers, s):
+    B, T, Hq, Dk = s["q"].shape
+    Hkv, Dv = s["v"].shape[2:]
+    args = dict(scale=s["scale"], initial_state=s["initial_d"], lengths=s["lengths_d"])
+    o, _ = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], **args)
+    want, _, mag, _ = ref.attention(s["q"], s["k"], s["v"], s["log_decay"], s["scale"], s["initial"], s["lengths"])
+    n = ref.attention_terms(T, Dk, Dv)
+    u = ref.unit("bf16")
+
+    def bound(value, magnitude, terms):
+        return u * np.abs(value) + (u * u + terms * 2.0 ** -24) * magnitude + 1e-37
+
+    close("o", o, want, bound(want, mag, n))
+    got = layers.linear_attention_backward(s["do_d"], s["q_d"], s["k_d"], s["v_d"], s["decay_d"],
+                                           dfinal_state=s["dfinal_d"], **args)
+    want, mag = ref.attention_backward(s["do"], s["q"], s["k"], s["v"], s["log_decay"], s["scale"], s["initial"],
+                                       s["lengths"], s["dfinal"])
+    n = ref.attention_terms(T * Hq // Hkv, Dk, Dv)
+    for name, g in zip(("dq", "dk", "dv"), got):
+        close(name, g, want[name], bound(want[name], mag[name], n))
