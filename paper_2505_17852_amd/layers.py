@@ -2,8 +2,9 @@
 linear attention with a decay for each head, layer norm and AdamW.
 
 Argument marshalling only: every computation runs in the library's HIP
-kernels, on the current torch stream unless one is passed. Outputs and
-workspaces are allocated by torch when they are not given. Errors: ValueError
+kernels, on the current torch stream unless one is passed (which then serves as the
+current one: the caller makes it wait for what it needs). Outputs and
+workspaces are allocated by torch, for the call's stream, when they are not given. Errors: ValueError
 for arguments that do not fit together, zo.ZoError for what the library refuses.
 
     layer_norm, layer_norm_backward
@@ -76,10 +77,8 @@ def _check(st: int):
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream, like: torch.Tensor):
-    """The raw stream of a call on like's device: the given one, or torch's current one."""
-    if stream is not None:
-        return stream.cuda_stream
+def _stream(like: torch.Tensor):
+    """torch's current raw stream on like's device."""
     if _current_stream is not None:
         return _current_stream(like.get_device())
     return torch.cuda.current_stream(like.device).cuda_stream
@@ -110,12 +109,24 @@ def _flat(t: torch.Tensor | None, name: str, dtype, shape, like: torch.Tensor):
     return t.data_ptr()
 
 
-def _on_stream(stream, *tensors):
-    """Tensors allocated here for a call on another stream than the current one belong to that stream."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+def _record(stream, values):
+    for x in values:
+        if isinstance(x, torch.Tensor):
+            x.record_stream(stream)
+        elif isinstance(x, (list, tuple)):
+            _record(stream, x)
+
+
+def _beside(stream, call, *args):
+    """call(*args) on another stream than the current one. What it allocates is allocated there: a block that was
+    freed on the current stream may still be in use by work queued on that. The tensors that it is given are held
+    until `stream` has done with them, those that it returns until the current stream has."""
+    here = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    _record(stream, args)
+    _record(here, out if isinstance(out, tuple) else (out,))
+    return out
 
 
 # ---- linear attention ----
@@ -186,6 +197,9 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     contiguous heads; log_decay fp32 [Hkv]; scale defaults to Dk ** -0.5; states fp32
     [B, Hkv, Dk, Dv]; lengths int32 [B] or None (all T). The final state is returned with
     return_state, or written into final_state (if that overlaps initial_state, its values are copied first)."""
+    if stream is not None:
+        return _beside(stream, linear_attention, q, k, v, log_decay, scale, initial_state, lengths, return_state, out,
+                       final_state, workspace)
     L = lib()
     B, T, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 4, scale)
     states = (B, Hkv, Dk, Dv)
@@ -196,14 +210,12 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
             final_state = torch.empty(states, dtype=f32, device=q.device)
     elif initial_state is not None and abs(final_state.data_ptr() - initial_state.data_ptr()) < 4 * B * Hkv * Dk * Dv:
         # (shared, or in part) the kernels read the one while they write the other
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(q.device)):
-            initial_state = initial_state.clone()
+        initial_state = initial_state.clone()
     ws, wp, wn = _workspace(workspace, L.zo_linear_attention_workspace_bytes(s, 0), q)
     _check(L.zo_linear_attention(
         s, hq, hk, hv, ho, _flat(log_decay, "log_decay", f32, (Hkv,), q),
         _flat(lengths, "lengths", torch.int32, (B,), q), _flat(initial_state, "initial_state", f32, states, q),
-        _flat(final_state, "final_state", f32, states, q), wp, wn, _stream(stream, q)))
-    _on_stream(stream, o, final_state, ws)
+        _flat(final_state, "final_state", f32, states, q), wp, wn, _stream(q)))
     return o, final_state
 
 
@@ -216,6 +228,9 @@ def linear_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor
     """Returns (dq, dk, dv, dinitial_state or None) for the output's gradient do
     [B, T, Hq, Dv] and the final state's dfinal_state (None: zeros), asynchronously.
     The initial state's gradient is computed when one was given, or as return_dinitial says."""
+    if stream is not None:
+        return _beside(stream, linear_attention_backward, do, q, k, v, log_decay, scale, initial_state, lengths,
+                       dfinal_state, return_dinitial, dq, dk, dv, workspace)
     L = lib()
     B, T, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 4, scale)
     states = (B, Hkv, Dk, Dv)
@@ -231,8 +246,7 @@ def linear_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor
         s, _heads(do, "do", (B, T, Hq, Dv), q), hq, hk, hv, hdq, hdk, hdv,
         _flat(log_decay, "log_decay", f32, (Hkv,), q), _flat(lengths, "lengths", torch.int32, (B,), q),
         _flat(initial_state, "initial_state", f32, states, q), _flat(dfinal_state, "dfinal_state", f32, states, q),
-        _flat(dinitial, "dinitial", f32, states, q), wp, wn, _stream(stream, q)))
-    _on_stream(stream, dq, dk, dv, dinitial, ws)
+        _flat(dinitial, "dinitial", f32, states, q), wp, wn, _stream(q)))
     return dq, dk, dv, dinitial
 
 
@@ -243,6 +257,8 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     [B, Hq, Dv] (asynchronous); state fp32 [n, Hkv, Dk, Dv] is updated in place. slots (int32
     [B], no two alike) names each sequence's state in it, -1 a sequence without one (its
     output is zero); None: sequence b's is state[b]."""
+    if stream is not None:
+        return _beside(stream, linear_attention_step, q, k, v, log_decay, state, scale, slots, out)
     L = lib()
     B, _, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 3, scale)
     n = state.shape[0]
@@ -252,9 +268,7 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     _check(L.zo_linear_attention_step(
         s, hq, hk, hv, ho, _flat(log_decay, "log_decay", torch.float32, (Hkv,), q),
         _flat(state, "state", torch.float32, (n, Hkv, Dk, Dv), q), n, _flat(slots, "slots", torch.int32, (B,), q),
-        _stream(stream, q)))
-    if stream is not None:
-        _on_stream(stream, o)
+        _stream(q)))
     return o
 
 
@@ -292,6 +306,8 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     """Layer norm over the last dimension: returns (y, mean, rstd), asynchronously; y of x's
     type and shape (out, which may be x, or a new tensor), mean and rstd fp32 [rows] for the
     backward pass. weight and bias [D], fp32 or bf16, or None."""
+    if stream is not None:
+        return _beside(stream, layer_norm, x, weight, bias, eps, out)
     L = lib()
     rows, D, xs = _rows(x, "x")
     wtype, w, b = _norm_params(weight, bias, D, x)
@@ -301,8 +317,7 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     mean = torch.empty(rows, dtype=torch.float32, device=dev)
     rstd = torch.empty(rows, dtype=torch.float32, device=dev)
     _check(L.zo_layer_norm(_DTYPES[x.dtype], wtype, rows, D, x.data_ptr(), xs, w, b, eps, y.data_ptr(), ys,
-                           mean.data_ptr(), rstd.data_ptr(), _stream(stream, x)))
-    _on_stream(stream, y, mean, rstd)
+                           mean.data_ptr(), rstd.data_ptr(), _stream(x)))
     return y, mean, rstd
 
 
@@ -315,6 +330,8 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
                         stream=None):
     """Returns (dx, dweight, dbias), asynchronously: dx of x's type and shape (out, which may
     be dy or x, or a new tensor), dweight and dbias fp32 [D], summed in a fixed order."""
+    if stream is not None:
+        return _beside(stream, layer_norm_backward, dy, x, weight, mean, rstd, out, workspace)
     L = lib()
     rows, D, xs = _rows(x, "x")
     dys = _rows(dy, "dy", x.shape, x)[2]
@@ -328,8 +345,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor 
     db = torch.empty(D, dtype=torch.float32, device=dev)
     ws, wp, wn = _workspace(workspace, L.zo_layer_norm_workspace_bytes(rows, D), x)
     _check(L.zo_layer_norm_backward(_DTYPES[x.dtype], wtype, rows, D, dy.data_ptr(), dys, x.data_ptr(), xs, w, mp, rp,
-                                    dx.data_ptr(), dxs, dw.data_ptr(), db.data_ptr(), wp, wn, _stream(stream, x)))
-    _on_stream(stream, dx, dw, db, ws)
+                                    dx.data_ptr(), dxs, dw.data_ptr(), db.data_ptr(), wp, wn, _stream(x)))
     return dx, dw, db
 
 
@@ -399,6 +415,9 @@ class AdamW:
         nothing, and skipped (device int32 [1]) is set to 1, else to 0. step_count goes up
         either way."""
         grads = list(grads)
+        if stream is not None:
+            _beside(stream, self.step, grads, grad_scale, skipped)
+            return _record(stream, (self.params, self._m, self._v, self._m_scale, self._v_scale))
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} tensors")
         like, params = self._m, self.params
@@ -423,16 +442,18 @@ class AdamW:
         _check(lib().zo_adamw(C.byref(cfg), self._table, len(grads), like.data_ptr(), self._v.data_ptr(),
                               self._m_scale.data_ptr() if eight else None,
                               self._v_scale.data_ptr() if eight else None,
-                              gs, sk, _stream(stream, like)))
+                              gs, sk, _stream(like)))
         self.step_count += 1
 
     def moments(self, stream=None):
         """The flat fp32 (m, v): the buffers themselves (32 bits), or the values that the codes stand for."""
         if self.state_bits == 32:
             return self.m, self.v
+        if stream is not None:
+            _record(stream, (self._m, self._v, self._m_scale, self._v_scale))
+            return _beside(stream, self.moments)
         m = torch.empty(self.m.numel(), dtype=torch.float32, device=self.m.device)
         v = torch.empty_like(m)
         _check(lib().zo_adamw_moments(m.numel(), self.m.data_ptr(), self.v.data_ptr(), self.m_scale.data_ptr(),
-                                      self.v_scale.data_ptr(), m.data_ptr(), v.data_ptr(), _stream(stream, m)))
-        _on_stream(stream, m, v)
+                                      self.v_scale.data_ptr(), m.data_ptr(), v.data_ptr(), _stream(m)))
         return m, v

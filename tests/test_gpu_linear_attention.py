@@ -446,3 +446,24 @@ def _near_fp32(layers, s):
     n = ref.attention_terms(T * Hq // Hkv, Dk, Dv)
     for name, g in zip(("dq", "dk", "dv"), got):
         close(name, g, want[name], bound(want[name], mag[name], n))
+
+
+def test_a_call_on_another_stream_takes_no_block_that_queued_work_still_uses(layers):
+    """Tensors of the outputs' size are freed while the current stream's work on them is pending; a call on another stream
+    gets other memory, and the right values."""
+    s = make(np.random.default_rng(61), "bf16", 2, 1024, 16, 16, 64, 64)
+    args = (s["q_d"], s["k_d"], s["v_d"], s["decay_d"])
+    want, _ = layers.linear_attention(*args)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy = [torch.zeros_like(want) for _ in range(3)]
+    freed = {b.data_ptr() for b in busy}
+    for b in busy:
+        for _ in range(200):
+            b.add_(1.0)
+    del busy, b
+    o, _ = layers.linear_attention(*args, stream=side)
+    side.synchronize()
+    assert o.data_ptr() not in freed and torch.equal(o, want)
+    torch.cuda.synchronize()
+    assert torch.equal(o, want)
