@@ -381,7 +381,7 @@ class AdamW:
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(self.params)
         if len(decay) != len(self.params):
             raise ValueError(f"{len(decay)} weight decays for {len(self.params)} tensors")
-        self.lr, self.betas, self.eps, self.state_bits, self.step_count = lr, tuple(betas), eps, state_bits, 0
+        self.lr, self.betas, self.eps, self._bits, self.step_count = lr, tuple(betas), eps, state_bits, 0
         self.offsets, at = [], 0
         for p in self.params:
             self.offsets.append(at)
@@ -403,7 +403,8 @@ class AdamW:
             *(_Tensor(p.data_ptr(), None, p.numel(), o, float(d), _DTYPES[p.dtype], zo.FP32)
               for p, o, d in zip(self.params, self.offsets, decay)))
 
-    # the kernels trust the buffers' sizes: they can be written into, not exchanged
+    # the kernels trust the buffers' types and sizes: they can be written into, not exchanged
+    state_bits = property(lambda self: self._bits)
     m = property(lambda self: self._m)
     v = property(lambda self: self._v)
     m_scale = property(lambda self: self._m_scale)
@@ -437,8 +438,8 @@ class AdamW:
             t.param, t.grad, t.gdtype = p, g, kind
         gs = _flat(grad_scale, "grad_scale", torch.float32, (1,), like)
         sk = _flat(skipped, "skipped", torch.int32, (1,), like)
-        cfg = _AdamWConfig(self.lr, self.betas[0], self.betas[1], self.eps, self.step_count + 1, self.state_bits)
-        eight = self.state_bits == 8
+        cfg = _AdamWConfig(self.lr, self.betas[0], self.betas[1], self.eps, self.step_count + 1, self._bits)
+        eight = self._bits == 8
         _check(lib().zo_adamw(C.byref(cfg), self._table, len(grads), like.data_ptr(), self._v.data_ptr(),
                               self._m_scale.data_ptr() if eight else None,
                               self._v_scale.data_ptr() if eight else None,
@@ -447,7 +448,7 @@ class AdamW:
 
     def moments(self, stream=None):
         """The flat fp32 (m, v): the buffers themselves (32 bits), or the values that the codes stand for."""
-        if self.state_bits == 32:
+        if self._bits == 32:
             return self.m, self.v
         if stream is not None:
             _record(stream, (self._m, self._v, self._m_scale, self._v_scale))
