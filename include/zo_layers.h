@@ -142,7 +142,9 @@ int zo_layer_norm_backward(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t
  *   m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2
  *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
  * The moments of all tensors lie in flat arrays; a tensor's begin at its
- * state_offset, a multiple of ZO_ADAMW_BLOCK, and take whole blocks.
+ * state_offset, a multiple of ZO_ADAMW_BLOCK, and take whole blocks. All tensors are updated
+ * at once: the parameters of two, or their moments, may not overlap (ZO_EINVAL; a tied
+ * tensor is given once, with the sum of its gradients).
  *   32 bits  m and v fp32
  *   8 bits   m int8 and v uint8 codes, and m_scale and v_scale fp32, the largest |m| and v of each
  *            block: a code c stands for m_scale sign(c) (c / 127)^2, or v_scale (c / 255)^4.

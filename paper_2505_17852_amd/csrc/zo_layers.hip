@@ -3,7 +3,9 @@
 // device memory.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "zo_error.hpp"
 #include "zo_layers.hpp"
@@ -70,6 +72,37 @@ int check_workspace(const zo_linattn* s, bool backward, const void* workspace, s
   if (!aligned16(workspace)) return fail(ZO_EINVAL, "workspace must be 16-byte aligned");
   return ZO_OK;
 }
+
+// Ranges [begin, end) of memory, to be checked for overlaps: one comparison each where they come in order (views of one
+// vector, moments one after another), sorted otherwise.
+class Ranges {
+ public:
+  explicit Ranges(int32_t n) : at_(n <= kFew ? few_ : (Range*)std::malloc(sizeof(Range) * (size_t)n)) {}
+  ~Ranges() {
+    if (at_ != few_) std::free(at_);
+  }
+  bool ready() const { return at_ != nullptr; }
+  void add(uint64_t begin, uint64_t bytes) { at_[n_++] = Range{begin, begin + bytes}; }
+  bool overlap() {
+    if (in_order()) return false;
+    std::sort(at_, at_ + n_, [](const Range& a, const Range& b) { return a.begin < b.begin; });
+    return !in_order();
+  }
+
+ private:
+  struct Range {
+    uint64_t begin, end;
+  };
+  static constexpr int32_t kFew = 64;
+  Range few_[kFew];
+  Range* at_;
+  int32_t n_ = 0;
+  bool in_order() const {
+    for (int32_t i = 1; i < n_; ++i)
+      if (at_[i].begin < at_[i - 1].end) return false;
+    return true;
+  }
+};
 
 }  // namespace
 
@@ -340,6 +373,8 @@ int zo_adamw(const zo_adamw_config* cfg, const zo_adamw_tensor* tensors, int32_t
   if (cfg->state_bits != 32 && cfg->state_bits != 8) return fail(ZO_EINVAL, "state_bits must be 32 or 8");
   if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return fail(ZO_EINVAL, "n_tensors < 0, or tensors is NULL");
   bool any = false;
+  Ranges params(n_tensors), moments(n_tensors);
+  if (!params.ready() || !moments.ready()) return fail(ZO_ENOMEM, "no host memory for %d tensors", n_tensors);
   for (int32_t i = 0; i < n_tensors; ++i) {
     const zo_adamw_tensor& t = tensors[i];
     if (t.n < 0 || t.n > (int64_t)1 << 40) return fail(ZO_EINVAL, "tensor %d: n must lie in [0, 2^40]", i);
@@ -350,8 +385,14 @@ int zo_adamw(const zo_adamw_config* cfg, const zo_adamw_tensor* tensors, int32_t
     if (t.state_offset < 0 || t.state_offset % ZO_ADAMW_BLOCK)
       return fail(ZO_EINVAL, "tensor %d: state_offset must be a multiple of %d", i, ZO_ADAMW_BLOCK);
     if (!std::isfinite(t.weight_decay)) return fail(ZO_EINVAL, "tensor %d: weight_decay must be finite", i);
-    any |= t.n > 0;
+    if (t.n == 0) continue;
+    any = true;
+    params.add((uint64_t)(uintptr_t)t.param, (uint64_t)t.n * type_bytes(t.pdtype));
+    moments.add((uint64_t)t.state_offset, (uint64_t)((t.n + ZO_ADAMW_BLOCK - 1) / ZO_ADAMW_BLOCK * ZO_ADAMW_BLOCK));
   }
+  // a launch updates all tensors in no order
+  if (params.overlap()) return fail(ZO_EINVAL, "the param buffers of two tensors overlap");
+  if (moments.overlap()) return fail(ZO_EINVAL, "the moments of two tensors overlap");
   if (any && (!m || !v)) return fail(ZO_EINVAL, "m or v is NULL");
   if (!aligned16(m) || !aligned16(v)) return fail(ZO_EINVAL, "m and v must be 16-byte aligned");
   if (cfg->state_bits == 8) {

@@ -358,7 +358,8 @@ _device_of, _contiguous, _address = torch.Tensor.get_device, torch.Tensor.is_con
 class AdamW:
     """AdamW over a list of parameter tensors, all in one launch for up to 64 of them.
 
-    params: contiguous device tensors, fp32 or bf16, updated in place. weight_decay: one
+    params: contiguous device tensors, fp32 or bf16, updated in place, that share no memory (a tied tensor
+    is given once, with the sum of its gradients). weight_decay: one
     number, or one for each tensor. state_bits: 32 (m and v fp32) or 8 (m int8 and v uint8
     codes with m_scale and v_scale, the largest values of blocks of 256: see
     zo_layers.h). The moments of tensor i begin at offsets[i] of the flat m and v and take
@@ -378,6 +379,11 @@ class AdamW:
             _device(p, f"params[{i}]", None, first)
             if not p.is_contiguous():
                 raise ValueError(f"params[{i}] must be contiguous")
+        ends = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size(), i)
+                      for i, p in enumerate(self.params) if p.numel())
+        for a, b in zip(ends, ends[1:]):
+            if b[0] < a[1]:
+                raise ValueError(f"params[{a[2]}] and params[{b[2]}] share memory: a tied tensor is given once")
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(self.params)
         if len(decay) != len(self.params):
             raise ValueError(f"{len(decay)} weight decays for {len(self.params)} tensors")
