@@ -122,6 +122,16 @@ __device__ __forceinline__ int encode_v(float v, float top, float inv) {
   return v > 0.0f ? max((int)code, 1) : 0;
 }
 
+// m / (sqrt(v) + eps). It is scaled by lr, far below the parameter: the approximate root and reciprocal serve. They
+// take subnormal numbers for zero, so small ones (and the quotient's sides alike) are scaled up by a power of two first.
+__device__ __forceinline__ float quotient(float m, float v, float eps) {
+#pragma clang fp contract(off)
+  const bool low = v < 0x1p-96f;
+  const float den = __builtin_amdgcn_sqrtf(low ? v * 0x1p64f : v) * (low ? 0x1p-32f : 1.0f) + eps;
+  const float up = den < 0x1p-64f ? 0x1p64f : 1.0f;
+  return (m * up) * __builtin_amdgcn_rcpf(den * up);
+}
+
 template <int bits>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const Args a) {
 #pragma clang fp contract(off)
@@ -168,9 +178,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Args a) {
     const float ge = a.grad_scale ? g[e] * gs : g[e];
     m[e] = m[e] * a.b1 + ge * a.omb1;
     v[e] = v[e] * a.b2 + (ge * ge) * a.omb2;
-    // (the quotient is scaled by lr, far below the parameter: the approximate root and reciprocal serve)
-    const float change = (m[e] * a.c1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e] * a.c2) + a.eps);
-    p[e] = p[e] * t.keep - change * a.lr;
+    p[e] = p[e] * t.keep - quotient(m[e] * a.c1, v[e] * a.c2, a.eps) * a.lr;
   }
   if (t.pbf) store8((uint16_t*)t.p + j, left, p);
   else store8((float*)t.p + j, left, p);

@@ -234,3 +234,26 @@ def test_gradients_that_do_not_fit_are_refused(layers):
     assert opt.step_count == 0
     opt.step(good)
     assert opt.step_count == 1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [0.0, 1e-40, 1e-25, 1e-18])
+def test_second_moments_and_denominators_below_the_normal_range(layers, eps, bits):
+    """First steps from gradients of 3e-20 to 1e-17, whose squares are subnormal or near it, and (but for eps = 0, where
+    the quotient has no value) zero. Roundings of the subnormal square and product are of 2^-150 each; with bias
+    correction the second moment is off by c2 (2^-150 (1 + 0.01) and 4 units), the change by what that makes of the
+    quotient and 8 units more."""
+    rng = np.random.default_rng(12)
+    g = (10.0 ** rng.uniform(np.log10(3e-20), -17, 3000) * rng.choice([-1, 1], 3000)).astype(np.float32)
+    if eps:
+        g[::7] = 0.0
+    p = torch.ones(3000, device="cuda")
+    opt = layers.AdamW([p], lr=LR, betas=BETAS, eps=eps, state_bits=bits)
+    opt.step([torch.from_numpy(g).cuda()])
+    e = float(np.float32(eps))
+    ge = g.astype(np.float64)
+    off = 1.02 * 2.0 ** -150 / (1 - BETAS[1]) + ref.ulps(4) * ge ** 2
+    lo, hi = (LR * np.abs(ge) / np.maximum(np.sqrt(np.maximum(ge ** 2 + s * off, 0)) + e, 1e-300) for s in (1, -1))
+    change = LR * np.abs(ge) / np.maximum(np.sqrt(ge ** 2) + e, 1e-300)
+    bound = np.maximum(change - lo, hi - change) + ref.ulps(8) * change + ref.ulps(2)
+    within("p", host(p), 1.0 - np.sign(ge) * change, bound)
