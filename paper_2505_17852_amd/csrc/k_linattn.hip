@@ -764,14 +764,14 @@ __global__ __launch_bounds__(kThreads) void linattn_few_kernel(LinCall c) {
     ys[p][d] = d < a.dx ? to_f32(y[t * a.y.t + (p % a.sources) * a.y.h + d]) : 0.0f;
   }
   __syncthreads();
-  const float gamma = decay(c.log_decay[kvh] * 1.44269504088896340736f, 1);
+  const Gamma gamma(c.log_decay[kvh]);
   for (int u = 0; u < n; ++u) {
     const int64_t t = a.reverse ? n - 1 - u : u;
     if (!a.reverse)
 #pragma unroll
       for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] *= gamma;
+        for (int e = 0; e < 4; ++e) s[i][e] = gamma.times(s[i][e], 0.0f);
     for (int q = 0; q < a.sources; ++q) {
       float zv[4];
 #pragma unroll
@@ -800,7 +800,7 @@ __global__ __launch_bounds__(kThreads) void linattn_few_kernel(LinCall c) {
 #pragma unroll
       for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] *= gamma;
+        for (int e = 0; e < 4; ++e) s[i][e] = gamma.times(s[i][e], 0.0f);
   }
   __syncthreads();
   for (int at = tid; at < c.T * 64; at += kThreads) {

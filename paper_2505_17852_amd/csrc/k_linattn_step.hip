@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinStep a) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) vs[e] = e < left ? to_f32(v[e]) : 0.0f;
   for (int d = tid; d < ROWS * kRowGroups; d += 256) ks[d] = d < a.dk ? to_f32(k[d]) : 0.0f;
-  const float gamma = __expf(a.log_decay[h]);
+  const Gamma gamma(a.log_decay[h]);
   for (int g0 = 0; g0 < groups; g0 += kHeads) {
     const int n = min(kHeads, groups - g0);
     for (int i = 0; i < n; ++i) {
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(LinStep a) {
       for (int i = 0; i < ROWS; ++i) {
         const int r = rg + kRowGroups * i;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] = fmaf(gamma, s[i][e], ks[r] * vs[e]);
+        for (int e = 0; e < 4; ++e) s[i][e] = gamma.times(s[i][e], ks[r] * vs[e]);
         if (r < a.dk && left >= 4) {
           store_run<float, 4>(S + (int64_t)r * a.dv, s[i]);
         } else {

@@ -82,6 +82,22 @@ __device__ __forceinline__ u4 drop(u4 v, int n) {
 
 // ---- linear attention (k_linattn.hip, k_linattn_step.hip) ----
 
+// gamma = high + low. A state that takes gamma at every token would drift by gamma's rounding, thousands of times half a
+// unit in the last place (6e-5 after 2,000 tokens), so it is held in two parts, from its value in 64 bits.
+struct Gamma {
+  float high, low;
+  __device__ __forceinline__ explicit Gamma(float log_decay) {
+    const double gamma = exp((double)log_decay);
+    high = (float)gamma;
+    low = high < __builtin_inff() ? (float)(gamma - (double)high) : 0.0f;
+  }
+  // gamma s + add, at any s (the lower part of an infinite one is left out)
+  __device__ __forceinline__ float times(float s, float add) const {
+    constexpr float kMax = 3.40282347e38f;
+    return fmaf(high, s, fmaf(low, __builtin_amdgcn_fmed3f(s, -kMax, kMax), add));
+  }
+};
+
 struct Heads {
   const void* p;
   int64_t b, t, h;  // strides in elements

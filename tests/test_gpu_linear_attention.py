@@ -467,3 +467,51 @@ def test_a_call_on_another_stream_takes_no_block_that_queued_work_still_uses(lay
     assert o.data_ptr() not in freed and torch.equal(o, want)
     torch.cuda.synchronize()
     assert torch.equal(o, want)
+
+
+@pytest.mark.parametrize("at_once", [0, 1, 4])
+def test_thousands_of_single_tokens_do_not_drift(layers, at_once):
+    """States that only decay, 2,000 tokens: each step rounds a value within 2^-24 of it. Where gamma's significand is full,
+    to either side as often, so that the mean over 16,384 values of a head is known to 6 sqrt(2000) 2^-24 / sqrt(3) / 128 =
+    7.3e-8 (bound 1.5e-7). Where gamma is 1 - 2^-b, one product in 2^b is a tie, which may always fall the same way, by
+    half a unit: 2000 2^-b 2^-24 more. A decay of half a unit in the last place off, at every token, would be 6e-5."""
+    rng = np.random.default_rng(71)
+    B, H, D, n = 4, 8, 64, 2000
+    state, start = rand(rng, (B, H, D, D))
+    ld = ref.log_decays(H, 6.0, 11.0)
+    zero = torch.zeros(B, H, D, device="cuda")
+    decay = torch.from_numpy(ld).cuda()
+    if at_once:  # as sequences of that many positions
+        zero, other = zero.unsqueeze(1).expand(B, at_once, H, D).contiguous(), torch.empty_like(state)
+        for _ in range(n // at_once):
+            layers.linear_attention(zero, zero, zero, decay, initial_state=state, final_state=other)
+            state, other = other, state
+    else:
+        for _ in range(n):
+            layers.linear_attention_step(zero, zero, zero, decay, state)
+    want = start.astype(np.float64) * np.exp(n * ld.astype(np.float64))[None, :, None, None]
+    off = (host(state) / want - 1.0).mean(axis=(0, 2, 3))
+    print(off, flush=True)
+    bits = np.linspace(6.0, 11.0, H)
+    ties = np.where(bits == np.round(bits), n * 2.0 ** -bits * 2.0 ** -24, 0.0)
+    assert (np.abs(off) <= 1.5e-7 + ties).all()
+
+
+@pytest.mark.parametrize("log_decay", [0.0, -float("inf"), -0.25, -0.75, -30.0, 0.25])
+def test_a_token_on_states_that_are_not_finite(layers, log_decay):
+    """Infinities stay what they are under a decay, NaN stays NaN, and the values beside them are as alone."""
+    rng = np.random.default_rng(72)
+    state, _ = rand(rng, (1, 1, 8, 8))
+    q, k, v = (rand(rng, (1, 1, 8))[0] for _ in range(3))
+    decay = torch.tensor([log_decay], device="cuda")
+    alone = state.clone()
+    layers.linear_attention_step(q, k, v, decay, alone)
+    state[0, 0, 2, 3], state[0, 0, 4, 5], state[0, 0, 6, 7] = float("inf"), -float("inf"), float("nan")
+    layers.linear_attention_step(q, k, v, decay, state)
+    bad = torch.zeros(8, 8, dtype=torch.bool, device="cuda")
+    bad[2, 3] = bad[4, 5] = bad[6, 7] = True
+    assert torch.equal(state[0, 0][~bad], alone[0, 0][~bad]) and torch.isnan(state[0, 0, 6, 7])
+    if log_decay > -float("inf"):
+        assert state[0, 0, 2, 3] == float("inf") and state[0, 0, 4, 5] == -float("inf")
+    else:
+        assert torch.isnan(state[0, 0, 2, 3]) and torch.isnan(state[0, 0, 4, 5])
