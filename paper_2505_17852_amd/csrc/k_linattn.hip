@@ -736,15 +736,24 @@ __global__ __launch_bounds__(kThreads) void linattn_few_kernel(LinCall c) {
   for (int i = 0; i < ROWS; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) s[i][e] = 0.0f;
+  // A state handed from call to call would drift by gamma's rounding: one of its n decays, as it is read (forward) or
+  // written (backward), takes gamma's lower part for all of them (at every position that takes a tenth more time).
+  float gamma = decay(c.log_decay[kvh] * 1.44269504088896340736f, 1), lower = 0.0f;
+  if (a.init) {
+    const Gamma both(c.log_decay[kvh]);
+    gamma = both.high;
+    lower = (float)n * both.low;
+  }
+  const auto aged = [&](float v, bool now) { return now ? fmaf(gamma, v, lower * finite(v)) : v; };
+  const bool before = n > 0 && !a.reverse, after = n > 0 && a.reverse;
   const bool whole = left >= 4 && !a.state_t;  // a thread's four values lie together
   if (a.init && whole) {
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) load_run<float, 4>(a.init + state_at + min(rg + GROUPS * i, a.dx - 1) * sx + col + c4, s[i]);
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
-      if (rg + GROUPS * i >= a.dx)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] = 0.0f;
+      for (int e = 0; e < 4; ++e) s[i][e] = rg + GROUPS * i < a.dx ? aged(s[i][e], before) : 0.0f;
   } else if (a.init) {
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
@@ -752,7 +761,7 @@ __global__ __launch_bounds__(kThreads) void linattn_few_kernel(LinCall c) {
       for (int e = 0; e < 4; ++e) {
         const int r = rg + GROUPS * i;
         const float v = a.init[state_at + min(r, a.dx - 1) * sx + min(col + c4 + e, a.dz - 1) * sz];
-        s[i][e] = r < a.dx && e < left ? v : 0.0f;
+        s[i][e] = r < a.dx && e < left ? aged(v, before) : 0.0f;
       }
   }
   for (int at = tid; at < n * DX; at += kThreads) {
@@ -764,14 +773,13 @@ __global__ __launch_bounds__(kThreads) void linattn_few_kernel(LinCall c) {
     ys[p][d] = d < a.dx ? to_f32(y[t * a.y.t + (p % a.sources) * a.y.h + d]) : 0.0f;
   }
   __syncthreads();
-  const Gamma gamma(c.log_decay[kvh]);
   for (int u = 0; u < n; ++u) {
     const int64_t t = a.reverse ? n - 1 - u : u;
-    if (!a.reverse)
+    if (before && u > 0)
 #pragma unroll
       for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] = gamma.times(s[i][e], 0.0f);
+        for (int e = 0; e < 4; ++e) s[i][e] *= gamma;
     for (int q = 0; q < a.sources; ++q) {
       float zv[4];
 #pragma unroll
@@ -796,11 +804,11 @@ __global__ __launch_bounds__(kThreads) void linattn_few_kernel(LinCall c) {
       acc[e] += __shfl_xor(acc[e], 32, 64);
       if ((tid & 63) < 16) part[u][tid >> 6][c4 + e] = acc[e];
     }
-    if (a.reverse)
+    if (after && u < n - 1)
 #pragma unroll
       for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] = gamma.times(s[i][e], 0.0f);
+        for (int e = 0; e < 4; ++e) s[i][e] *= gamma;
   }
   __syncthreads();
   for (int at = tid; at < c.T * 64; at += kThreads) {
@@ -810,11 +818,16 @@ __global__ __launch_bounds__(kThreads) void linattn_few_kernel(LinCall c) {
     out[t * a.ot + d] = from_f32<T>(
         u < n ? a.carry * ((part[u][0][d] + part[u][1][d]) + (part[u][2][d] + part[u][3][d])) : 0.0f);
   }
-  if (a.fin && h == kvh * a.heads && whole) {
+  if (!a.fin || h != kvh * a.heads) return;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[i][e] = aged(s[i][e], after);
+  if (whole) {
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
       if (rg + GROUPS * i < a.dx) store_run<float, 4>(a.fin + state_at + (rg + GROUPS * i) * sx + col + c4, s[i]);
-  } else if (a.fin && h == kvh * a.heads) {
+  } else {
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
 #pragma unroll

@@ -82,6 +82,12 @@ __device__ __forceinline__ u4 drop(u4 v, int n) {
 
 // ---- linear attention (k_linattn.hip, k_linattn_step.hip) ----
 
+// The nearest finite value: an infinite state takes no correction (which would make it NaN).
+__device__ __forceinline__ float finite(float s) {
+  constexpr float kMax = 3.40282347e38f;
+  return __builtin_amdgcn_fmed3f(s, -kMax, kMax);
+}
+
 // gamma = high + low. A state that takes gamma at every token would drift by gamma's rounding, thousands of times half a
 // unit in the last place (6e-5 after 2,000 tokens), so it is held in two parts, from its value in 64 bits.
 struct Gamma {
@@ -91,11 +97,8 @@ struct Gamma {
     high = (float)gamma;
     low = high < __builtin_inff() ? (float)(gamma - (double)high) : 0.0f;
   }
-  // gamma s + add, at any s (the lower part of an infinite one is left out)
-  __device__ __forceinline__ float times(float s, float add) const {
-    constexpr float kMax = 3.40282347e38f;
-    return fmaf(high, s, fmaf(low, __builtin_amdgcn_fmed3f(s, -kMax, kMax), add));
-  }
+  // gamma s + add
+  __device__ __forceinline__ float times(float s, float add) const { return fmaf(high, s, fmaf(low, finite(s), add)); }
 };
 
 struct Heads {

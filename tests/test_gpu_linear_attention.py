@@ -497,17 +497,26 @@ def test_thousands_of_single_tokens_do_not_drift(layers, at_once):
     assert (np.abs(off) <= 1.5e-7 + ties).all()
 
 
+@pytest.mark.parametrize("at_once", [0, 1])
 @pytest.mark.parametrize("log_decay", [0.0, -float("inf"), -0.25, -0.75, -30.0, 0.25])
-def test_a_token_on_states_that_are_not_finite(layers, log_decay):
+def test_a_token_on_states_that_are_not_finite(layers, log_decay, at_once):
     """Infinities stay what they are under a decay, NaN stays NaN, and the values beside them are as alone."""
     rng = np.random.default_rng(72)
     state, _ = rand(rng, (1, 1, 8, 8))
     q, k, v = (rand(rng, (1, 1, 8))[0] for _ in range(3))
     decay = torch.tensor([log_decay], device="cuda")
+
+    def token(state):
+        if at_once:
+            layers.linear_attention(q.unsqueeze(1), k.unsqueeze(1), v.unsqueeze(1), decay, initial_state=state,
+                                    final_state=state)
+        else:
+            layers.linear_attention_step(q, k, v, decay, state)
+
     alone = state.clone()
-    layers.linear_attention_step(q, k, v, decay, alone)
+    token(alone)
     state[0, 0, 2, 3], state[0, 0, 4, 5], state[0, 0, 6, 7] = float("inf"), -float("inf"), float("nan")
-    layers.linear_attention_step(q, k, v, decay, state)
+    token(state)
     bad = torch.zeros(8, 8, dtype=torch.bool, device="cuda")
     bad[2, 3] = bad[4, 5] = bad[6, 7] = True
     assert torch.equal(state[0, 0][~bad], alone[0, 0][~bad]) and torch.isnan(state[0, 0, 6, 7])
