@@ -50,7 +50,7 @@ extern "C" {
 
 typedef struct {
     int32_t batch;      /* sequences, >= 0 */
-    int32_t length;     /* positions, 0 .. 2^30 (the step: ignored) */
+    int32_t length;     /* positions, 0 .. 2^30 (the step takes one, whatever this says within the range) */
     int32_t q_heads;    /* a multiple of kv_heads */
     int32_t kv_heads;   /* > 0 */
     int32_t key_dim;    /* 1 .. ZO_LINATTN_MAX_DIM */
@@ -62,7 +62,7 @@ typedef struct {
 /* A tensor [batch][length][heads][dim]: element (b, t, h, d) at
  * data[b * batch_stride + t * position_stride + h * head_stride + d], strides
  * in elements, any sign (position_stride within
- * ZO_LINATTN_MAX_STRIDE). Any alignment of data that its type needs. Inputs may
+ * ZO_LINATTN_MAX_STRIDE; not used where there is one position or none). Any alignment of data that its type needs. Inputs may
  * overlap (slices of one projection); an output may overlap nothing. */
 typedef struct {
     void* data;
@@ -103,7 +103,7 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
                                  void* workspace, size_t ws_bytes, void* stream);
 
 /* One token for each of B sequences, their states updated in place.
- * shape->length and the tensors' position strides are ignored. state is a pool
+ * shape->length and the tensors' position strides are not used. state is a pool
  * of n_slots states [n_slots][kv_heads][key_dim][value_dim]; sequence b's is
  * slots[b] (device int32; no two alike), or b itself where slots is NULL
  * (n_slots >= B then). A slot of -1 is a sequence without a state: its output is

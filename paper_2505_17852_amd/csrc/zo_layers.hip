@@ -39,19 +39,20 @@ int check_linattn(const zo_linattn* s) {
   return ZO_OK;
 }
 
-// A tensor that is read or written (its elements exist when `any`).
-int check_heads(const zo_heads* h, const char* name, int32_t dtype, bool any) {
+// A tensor of `positions` positions that is read or written (its elements exist when `any`).
+int check_heads(const zo_heads* h, const char* name, int32_t dtype, bool any, int32_t positions) {
   if (!h) return fail(ZO_EINVAL, "%s is NULL", name);
   if (any && !h->data) return fail(ZO_EINVAL, "%s has no data", name);
   if (!aligned_for(h->data, dtype)) return fail(ZO_EINVAL, "%s is not aligned to its type", name);
-  // the kernels reach the 64 positions of a chunk with 32-bit offsets
+  // the kernels reach the 64 positions of a chunk with 32-bit offsets; one position, or none, has no distance
+  if (positions < 2) return ZO_OK;
   if (h->position_stride > ZO_LINATTN_MAX_STRIDE || h->position_stride < -ZO_LINATTN_MAX_STRIDE)
     return fail(ZO_ESHAPE, "%s: position strides must stay within 2^24", name);
   return ZO_OK;
 }
 
-zo::Heads heads(const zo_heads* h) {
-  return zo::Heads{h->data, h->batch_stride, h->position_stride, h->head_stride};
+zo::Heads heads(const zo_heads* h, int32_t positions) {
+  return zo::Heads{h->data, h->batch_stride, positions < 2 ? 0 : h->position_stride, h->head_stride};
 }
 
 int check_state(const float* s, const char* name) {
@@ -122,8 +123,8 @@ int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_hea
   if (st) return st;
   const zo_linattn& s = *shape;
   const bool any = s.batch > 0 && s.length > 0;
-  if ((st = check_heads(q, "q", s.dtype, any)) || (st = check_heads(k, "k", s.dtype, any)) ||
-      (st = check_heads(v, "v", s.dtype, any)) || (st = check_heads(o, "o", s.dtype, any)) ||
+  if ((st = check_heads(q, "q", s.dtype, any, s.length)) || (st = check_heads(k, "k", s.dtype, any, s.length)) ||
+      (st = check_heads(v, "v", s.dtype, any, s.length)) || (st = check_heads(o, "o", s.dtype, any, s.length)) ||
       (st = check_state(log_decay, "log_decay")) || (st = check_state(initial_state, "initial_state")) ||
       (st = check_state(final_state, "final_state")) || (st = check_workspace(shape, false, workspace, ws_bytes)))
     return st;
@@ -133,12 +134,12 @@ int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_hea
     return fail(ZO_EINVAL, "final_state and initial_state must be different buffers");
   zo::LinCall c{};
   zo::LinPass& p = c.pass[0];
-  p.x = heads(q);
-  p.y = heads(k);
-  p.z = heads(v);
+  p.x = heads(q, s.length);
+  p.y = heads(k, s.length);
+  p.z = heads(v, s.length);
   p.out = o->data;
   p.ob = o->batch_stride;
-  p.ot = o->position_stride;
+  p.ot = s.length < 2 ? 0 : o->position_stride;
   p.oh = o->head_stride;
   p.dx = s.key_dim;
   p.dz = s.value_dim;
@@ -170,10 +171,10 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
   if (st) return st;
   const zo_linattn& s = *shape;
   const bool any = s.batch > 0 && s.length > 0;
-  if ((st = check_heads(dout, "dout", s.dtype, any)) || (st = check_heads(q, "q", s.dtype, any)) ||
-      (st = check_heads(k, "k", s.dtype, any)) || (st = check_heads(v, "v", s.dtype, any)) ||
-      (st = check_heads(dq, "dq", s.dtype, any)) || (st = check_heads(dk, "dk", s.dtype, any)) ||
-      (st = check_heads(dv, "dv", s.dtype, any)) || (st = check_state(log_decay, "log_decay")) ||
+  if ((st = check_heads(dout, "dout", s.dtype, any, s.length)) || (st = check_heads(q, "q", s.dtype, any, s.length)) ||
+      (st = check_heads(k, "k", s.dtype, any, s.length)) || (st = check_heads(v, "v", s.dtype, any, s.length)) ||
+      (st = check_heads(dq, "dq", s.dtype, any, s.length)) || (st = check_heads(dk, "dk", s.dtype, any, s.length)) ||
+      (st = check_heads(dv, "dv", s.dtype, any, s.length)) || (st = check_state(log_decay, "log_decay")) ||
       (st = check_state(initial_state, "initial_state")) || (st = check_state(dfinal_state, "dfinal_state")) ||
       (st = check_state(dinitial_state, "dinitial_state")) ||
       (st = check_workspace(shape, true, workspace, ws_bytes)))
@@ -186,12 +187,12 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
   zo::LinCall c{};
   // dq: forward in time, the transposed state
   zo::LinPass& a = c.pass[0];
-  a.x = heads(dout);
-  a.y = heads(v);
-  a.z = heads(k);
+  a.x = heads(dout, s.length);
+  a.y = heads(v, s.length);
+  a.z = heads(k, s.length);
   a.out = dq->data;
   a.ob = dq->batch_stride;
-  a.ot = dq->position_stride;
+  a.ot = s.length < 2 ? 0 : dq->position_stride;
   a.oh = dq->head_stride;
   a.dx = s.value_dim;
   a.dz = s.key_dim;
@@ -203,12 +204,12 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
   a.init = initial_state;
   // dv: backward in time, the gradient of the state
   zo::LinPass& d = c.pass[1];
-  d.x = heads(k);
-  d.y = heads(q);
-  d.z = heads(dout);
+  d.x = heads(k, s.length);
+  d.y = heads(q, s.length);
+  d.z = heads(dout, s.length);
   d.out = dv->data;
   d.ob = dv->batch_stride;
-  d.ot = dv->position_stride;
+  d.ot = s.length < 2 ? 0 : dv->position_stride;
   d.oh = dv->head_stride;
   d.dx = s.key_dim;
   d.dz = s.value_dim;
@@ -222,12 +223,12 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
   // dk: backward in time, its transpose
   zo::LinPass& e = c.pass[2];
   e = d;
-  e.x = heads(v);
-  e.y = heads(dout);
-  e.z = heads(q);
+  e.x = heads(v, s.length);
+  e.y = heads(dout, s.length);
+  e.z = heads(q, s.length);
   e.out = dk->data;
   e.ob = dk->batch_stride;
-  e.ot = dk->position_stride;
+  e.ot = s.length < 2 ? 0 : dk->position_stride;
   e.oh = dk->head_stride;
   e.dx = s.value_dim;
   e.dz = s.key_dim;
@@ -253,8 +254,8 @@ int zo_linear_attention_step(const zo_linattn* shape, const zo_heads* q, const z
   if (st) return st;
   const zo_linattn& s = *shape;
   const bool any = s.batch > 0;
-  if ((st = check_heads(q, "q", s.dtype, any)) || (st = check_heads(k, "k", s.dtype, any)) ||
-      (st = check_heads(v, "v", s.dtype, any)) || (st = check_heads(o, "o", s.dtype, any)) ||
+  if ((st = check_heads(q, "q", s.dtype, any, 1)) || (st = check_heads(k, "k", s.dtype, any, 1)) ||
+      (st = check_heads(v, "v", s.dtype, any, 1)) || (st = check_heads(o, "o", s.dtype, any, 1)) ||
       (st = check_state(log_decay, "log_decay")) || (st = check_state(state, "state")))
     return st;
   if (!log_decay || (!state && n_slots > 0)) return fail(ZO_EINVAL, "a required pointer is NULL");
@@ -262,9 +263,9 @@ int zo_linear_attention_step(const zo_linattn* shape, const zo_heads* q, const z
     return fail(ZO_EINVAL, "n_slots (%d) must be >= 0, and >= batch (%d) without slots", n_slots, s.batch);
   if (((uintptr_t)slots & 3u) != 0) return fail(ZO_EINVAL, "slots is not aligned to its type");
   zo::LinStep a{};
-  a.q = heads(q);
-  a.k = heads(k);
-  a.v = heads(v);
+  a.q = heads(q, 1);
+  a.k = heads(k, 1);
+  a.v = heads(v, 1);
   a.o = o->data;
   a.ob = o->batch_stride;
   a.oh = o->head_stride;

@@ -524,3 +524,29 @@ def test_a_token_on_states_that_are_not_finite(layers, log_decay, at_once):
         assert state[0, 0, 2, 3] == float("inf") and state[0, 0, 4, 5] == -float("inf")
     else:
         assert torch.isnan(state[0, 0, 2, 3]) and torch.isnan(state[0, 0, 4, 5])
+
+
+def test_one_position_at_any_distance(layers):
+    """The distance between positions is free where there is one, or none: in the binding, and in a step's tensors."""
+    B, H, D = 3, 2, 32
+    s = make(np.random.default_rng(81), "f32", B, 1, H, H, D, D, True)
+    want = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], initial_state=s["initial_d"],
+                                   return_state=True)
+    far = [s[n + "_d"].as_strided((B, 1, H, D), (H * D, 1 << 40, D, 1)) for n in ("q", "k", "v", "do")]
+    out = torch.empty(B, 1, H, D, device="cuda").as_strided((B, 1, H, D), (H * D, 1 << 30, D, 1))
+    o, final = layers.linear_attention(*far[:3], s["decay_d"], initial_state=s["initial_d"], return_state=True, out=out)
+    assert torch.equal(o, want[0]) and torch.equal(final, want[1])
+    grads = layers.linear_attention_backward(s["do_d"], s["q_d"], s["k_d"], s["v_d"], s["decay_d"])
+    got = layers.linear_attention_backward(far[3], *far[:3], s["decay_d"])
+    assert all(torch.equal(a, b) for a, b in zip(got[:3], grads[:3]))
+    none = [x[:, :0] for x in far[:3]]
+    assert layers.linear_attention(*none, s["decay_d"])[0].shape == (B, 0, H, D)
+    state, o1 = s["initial_d"].clone(), torch.empty(B, H, D, device="cuda")
+    heads = [layers._HEADS.pack(t.data_ptr(), H * D, 1 << 40, D) for t in (s["q_d"], s["k_d"], s["v_d"], o1)]
+    shape = layers._SHAPE.pack(B, 0, H, H, D, D, 0, s["scale"])
+    layers._check(layers.lib().zo_linear_attention_step(shape, *heads, s["decay_d"].data_ptr(), state.data_ptr(), B,
+                                                        None, layers._stream(o1)))
+    n = ref.attention_terms(1, D, D)
+    wo, wfinal, mag, fmag = ref.attention(s["q"], s["k"], s["v"], s["log_decay"], s["scale"], s["initial"])
+    close("o", o1, wo[:, 0], ref.unit("f32") * np.abs(wo[:, 0]) + n * 2.0 ** -24 * mag[:, 0] + 1e-37)
+    close("state", state, wfinal, ref.state_bound(fmag, "f32", n))
