@@ -63,7 +63,9 @@ typedef struct {
  * data[b * batch_stride + t * position_stride + h * head_stride + d], strides
  * in elements, any sign (position_stride within
  * ZO_LINATTN_MAX_STRIDE; not used where there is one position or none). Any alignment of data that its type needs. Inputs may
- * overlap (slices of one projection); an output may overlap nothing. */
+ * overlap (slices of one projection); an output may share no value with them or
+ * another output (ZO_EINVAL where that is certain: the same first value, both without gaps,
+ * or the same strides). */
 typedef struct {
     void* data;
     int64_t batch_stride, position_stride, head_stride;
@@ -120,7 +122,8 @@ int zo_linear_attention_step(const zo_linattn* shape, const zo_heads* q, const z
  *   y = (x - mean) rstd w + b
  * xdtype is the type of x and y (and dy, dx), wdtype that of weight and bias;
  * weight and bias may be NULL (1 and 0). mean and rstd: device fp32 [rows],
- * kept for the backward pass, or both NULL. y may be x. */
+ * kept for the backward pass, or both NULL. y may be x with its stride (ZO_EINVAL if they
+ * share memory in another way). */
 int zo_layer_norm(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t D, const void* x, int64_t x_stride,
                   const void* weight, const void* bias, float eps, void* y, int64_t y_stride, float* mean,
                   float* rstd, void* stream);
@@ -131,7 +134,7 @@ size_t zo_layer_norm_workspace_bytes(int64_t rows, int64_t D);
 /* xhat = (x - mean) rstd, g = dy w:
  *   dx = rstd (g - avg(g) - xhat avg(g xhat));  dweight = sum_rows dy xhat;  dbias = sum_rows dy
  * dweight, dbias: device fp32 [D], each may be NULL (not wanted). Their sums run
- * in a fixed order: the same call gives the same bits. dx may be dy or x. */
+ * in a fixed order: the same call gives the same bits. dx may be dy or x, with its stride. */
 int zo_layer_norm_backward(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t D, const void* dy,
                            int64_t dy_stride, const void* x, int64_t x_stride, const void* weight,
                            const float* mean, const float* rstd, void* dx, int64_t dx_stride, float* dweight,

@@ -6,6 +6,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>
+#include <initializer_list>
+#include <utility>
 
 #include "zo_error.hpp"
 #include "zo_layers.hpp"
@@ -74,6 +76,106 @@ int check_workspace(const zo_linattn* s, bool backward, const void* workspace, s
   return ZO_OK;
 }
 
+// A tensor in memory: size[i] values stride[i] apart in each dimension; those of size 1 are left out.
+struct Strided {
+  static constexpr int kDims = 4;
+  const char* name;
+  uintptr_t data;
+  int64_t element;
+  int dims = 0;
+  int64_t size[kDims], stride[kDims];
+  bool empty = false;
+  uintptr_t begin, end;  // of the memory between its first and its last value
+
+  Strided(const char* n, const void* p, int32_t type, std::initializer_list<std::pair<int64_t, int64_t>> all)
+      : name(n), data((uintptr_t)p), element((int64_t)type_bytes(type)) {
+    begin = data;
+    end = data + (uintptr_t)element;
+    for (const auto& d : all) {
+      if (d.first == 0) empty = true;
+      if (d.first < 2) continue;
+      size[dims] = d.first;
+      stride[dims++] = d.second;
+      const uintptr_t reach = (uintptr_t)(d.first - 1) * (uintptr_t)d.second * (uintptr_t)element;
+      (d.second < 0 ? begin : end) += reach;
+    }
+    for (int i = 1; i < dims; ++i)  // by distance, the nearest first
+      for (int j = i; j > 0 && std::abs(stride[j]) < std::abs(stride[j - 1]); --j) {
+        std::swap(stride[j], stride[j - 1]);
+        std::swap(size[j], size[j - 1]);
+      }
+  }
+  // Every value between the first and the last belongs to it.
+  bool dense() const {
+    int64_t next = 1;
+    for (int i = 0; i < dims; ++i) {
+      if (std::abs(stride[i]) != next) return false;
+      next *= size[i];
+    }
+    return true;
+  }
+  bool in_one_place() const {
+    for (int i = 0; i < dims; ++i)
+      if (stride[i] == 0) return true;
+    return false;
+  }
+};
+
+// Whether sum_i x_i stride_i = distance for some x_i within (-b.size_i, a.size_i), i < dims.
+bool meet(const Strided& a, const Strided& b, int dims, int64_t distance, int* tries) {
+  if (dims == 0) return distance == 0;
+  if (--*tries < 0) return false;
+  const int i = dims - 1;
+  int64_t low = 0, high = 0;  // what the nearer dimensions can add
+  for (int j = 0; j < i; ++j) {
+    const int64_t x = (a.size[j] - 1) * a.stride[j], y = (b.size[j] - 1) * a.stride[j];
+    low -= std::max(y, -x);
+    high += std::max(x, -y);
+  }
+  const int64_t s = a.stride[i];
+  int64_t from = (distance - high) / s - 1, to = (distance - low) / s + 1;
+  if (from > to) std::swap(from, to);
+  from = std::max(from - 1, -(b.size[i] - 1));
+  to = std::min(to + 1, a.size[i] - 1);
+  for (int64_t x = from; x <= to && *tries >= 0; ++x) {
+    const int64_t left = distance - x * s;
+    if (left >= low && left <= high && meet(a, b, i, left, tries)) return true;
+  }
+  return false;
+}
+
+// Whether two tensors are known to share a value: they begin at the same one, both fill the memory that they span, or
+// their strides are the same (slices of one buffer). Others whose spans cross may lie between each other's values.
+bool share(const Strided& a, const Strided& b) {
+  if (a.empty || b.empty || a.begin >= b.end || b.begin >= a.end) return false;
+  if (a.data == b.data || (a.dense() && b.dense())) return true;
+  if (a.dims != b.dims || a.element != b.element) return false;
+  for (int i = 0; i < a.dims; ++i)
+    if (a.stride[i] != b.stride[i] || a.stride[i] == 0) return false;
+  int tries = 1024;  // (nested strides take a few)
+  return meet(a, b, a.dims, ((int64_t)(b.data - a.data)) / a.element, &tries);
+}
+
+// Outputs share nothing with inputs, with one another, or within themselves.
+int check_apart(std::initializer_list<Strided> outputs, std::initializer_list<Strided> inputs) {
+  for (const Strided* o = outputs.begin(); o != outputs.end(); ++o) {
+    if (!o->empty && o->in_one_place()) return fail(ZO_EINVAL, "%s: values of an output lie in one place (stride 0)", o->name);
+    for (const Strided& x : inputs)
+      if (share(*o, x)) return fail(ZO_EINVAL, "%s and %s share memory", o->name, x.name);
+    for (const Strided* p = outputs.begin(); p != o; ++p)
+      if (share(*o, *p)) return fail(ZO_EINVAL, "%s and %s share memory", o->name, p->name);
+  }
+  return ZO_OK;
+}
+
+Strided strided(const char* name, const zo_heads* h, const zo_linattn& s, int32_t positions, bool query, bool key) {
+  return Strided(name, h->data, s.dtype,
+                 {{s.batch, h->batch_stride},
+                  {positions, h->position_stride},
+                  {query ? s.q_heads : s.kv_heads, h->head_stride},
+                  {key ? s.key_dim : s.value_dim, 1}});
+}
+
 // Ranges [begin, end) of memory, to be checked for overlaps: one comparison each where they come in order (views of one
 // vector, moments one after another), sorted otherwise.
 class Ranges {
@@ -132,6 +234,10 @@ int zo_linear_attention(const zo_linattn* shape, const zo_heads* q, const zo_hea
   if (((uintptr_t)lengths & 3u) != 0) return fail(ZO_EINVAL, "lengths is not aligned to its type");
   if (overlap(s, final_state, initial_state))
     return fail(ZO_EINVAL, "final_state and initial_state must be different buffers");
+  if ((st = check_apart({strided("o", o, s, s.length, true, false)},
+                        {strided("q", q, s, s.length, true, true), strided("k", k, s, s.length, false, true),
+                         strided("v", v, s, s.length, false, false)})))
+    return st;
   zo::LinCall c{};
   zo::LinPass& p = c.pass[0];
   p.x = heads(q, s.length);
@@ -183,6 +289,11 @@ int zo_linear_attention_backward(const zo_linattn* shape, const zo_heads* dout, 
   if (((uintptr_t)lengths & 3u) != 0) return fail(ZO_EINVAL, "lengths is not aligned to its type");
   if (overlap(s, dinitial_state, dfinal_state))
     return fail(ZO_EINVAL, "dinitial_state and dfinal_state must be different buffers");
+  if ((st = check_apart({strided("dq", dq, s, s.length, true, true), strided("dk", dk, s, s.length, false, true),
+                         strided("dv", dv, s, s.length, false, false)},
+                        {strided("dout", dout, s, s.length, true, false), strided("q", q, s, s.length, true, true),
+                         strided("k", k, s, s.length, false, true), strided("v", v, s, s.length, false, false)})))
+    return st;
   const int share = s.q_heads / s.kv_heads;
   zo::LinCall c{};
   // dq: forward in time, the transposed state
@@ -262,6 +373,10 @@ int zo_linear_attention_step(const zo_linattn* shape, const zo_heads* q, const z
   if (n_slots < 0 || (!slots && n_slots < s.batch))
     return fail(ZO_EINVAL, "n_slots (%d) must be >= 0, and >= batch (%d) without slots", n_slots, s.batch);
   if (((uintptr_t)slots & 3u) != 0) return fail(ZO_EINVAL, "slots is not aligned to its type");
+  if ((st = check_apart({strided("o", o, s, 1, true, false)}, {strided("q", q, s, 1, true, true),
+                                                               strided("k", k, s, 1, false, true),
+                                                               strided("v", v, s, 1, false, false)})))
+    return st;
   zo::LinStep a{};
   a.q = heads(q, 1);
   a.k = heads(k, 1);
@@ -291,6 +406,14 @@ static int check_norm(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t D) {
   return ZO_OK;
 }
 
+// Rows out over rows in: the same ones, or apart.
+static int check_rows(const char* out, const void* y, int64_t ys, const char* in, const void* x, int64_t xs, int32_t type,
+                      int64_t rows, int64_t D) {
+  const bool same = y == x && (ys == xs || rows < 2);
+  const Strided o(out, y, type, {{rows, ys}, {D, 1}}), i(in, x, type, {{rows, xs}, {D, 1}});
+  return same ? check_apart({o}, {}) : check_apart({o}, {i});
+}
+
 int zo_layer_norm(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t D, const void* x, int64_t x_stride,
                   const void* weight, const void* bias, float eps, void* y, int64_t y_stride, float* mean,
                   float* rstd, void* stream) {
@@ -303,6 +426,7 @@ int zo_layer_norm(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t D, const
   if (!aligned_for(x, xdtype) || !aligned_for(y, xdtype) || !aligned_for(weight, wdtype) ||
       !aligned_for(bias, wdtype) || !aligned4(mean) || !aligned4(rstd))
     return fail(ZO_EINVAL, "a buffer is not aligned to its type");
+  if ((st = check_rows("y", y, y_stride, "x", x, x_stride, xdtype, rows, D))) return st;
   zo::NormArgs a{};
   a.xdtype = xdtype;
   a.wdtype = wdtype;
@@ -342,6 +466,9 @@ int zo_layer_norm_backward(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t
     if (need && !workspace) return fail(ZO_EINVAL, "workspace is NULL");
     if (!aligned16(workspace)) return fail(ZO_EINVAL, "workspace must be 16-byte aligned");
   }
+  if ((st = check_rows("dx", dx, dx_stride, "dy", dy, dy_stride, xdtype, rows, D)) ||
+      (st = check_rows("dx", dx, dx_stride, "x", x, x_stride, xdtype, rows, D)))
+    return st;
   zo::NormArgs a{};
   a.xdtype = xdtype;
   a.wdtype = wdtype;

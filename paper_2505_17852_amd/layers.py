@@ -196,7 +196,8 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     q [B, T, Hq, Dk], k [B, T, Hkv, Dk], v [B, T, Hkv, Dv] fp32 or bf16, any strides with
     contiguous heads; log_decay fp32 [Hkv]; scale defaults to Dk ** -0.5; states fp32
     [B, Hkv, Dk, Dv]; lengths int32 [B] or None (all T). The final state is returned with
-    return_state, or written into final_state (if that overlaps initial_state, its values are copied first)."""
+    return_state, or written into final_state (if that overlaps initial_state, its values are copied first).
+    out may lie in any strides, but shares no memory with q, k and v."""
     if stream is not None:
         return _beside(stream, linear_attention, q, k, v, log_decay, scale, initial_state, lengths, return_state, out,
                        final_state, workspace)
@@ -227,7 +228,8 @@ def linear_attention_backward(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor
                               dv: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
     """Returns (dq, dk, dv, dinitial_state or None) for the output's gradient do
     [B, T, Hq, Dv] and the final state's dfinal_state (None: zeros), asynchronously.
-    The initial state's gradient is computed when one was given, or as return_dinitial says."""
+    The initial state's gradient is computed when one was given, or as return_dinitial says.
+    dq, dk and dv (slices of one buffer, if wanted) share no memory with the inputs."""
     if stream is not None:
         return _beside(stream, linear_attention_backward, do, q, k, v, log_decay, scale, initial_state, lengths,
                        dfinal_state, return_dinitial, dq, dk, dv, workspace)
@@ -256,7 +258,7 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     """One token for each of B sequences: q [B, Hq, Dk], k [B, Hkv, Dk], v [B, Hkv, Dv] -> o
     [B, Hq, Dv] (asynchronous); state fp32 [n, Hkv, Dk, Dv] is updated in place. slots (int32
     [B], no two alike) names each sequence's state in it, -1 a sequence without one (its
-    output is zero); None: sequence b's is state[b]."""
+    output is zero); None: sequence b's is state[b]. out shares no memory with q, k and v."""
     if stream is not None:
         return _beside(stream, linear_attention_step, q, k, v, log_decay, state, scale, slots, out)
     L = lib()

@@ -201,3 +201,20 @@ def test_constant_rows_whose_mean_times_rstd_overflows(layers, D):
     want = r * (g - g.mean(1, keepdims=True))
     close("dx", dx, want, 43 * ref.unit("f32") * r * (np.abs(g) + np.abs(g).mean(1, keepdims=True)))
     assert not dw.any() and torch.isfinite(db).all()
+
+
+def test_rows_between_the_input_s_rows(layers):
+    """Input, output and gradient as columns of one buffer share no value, and are taken; shifted by one they are refused."""
+    from paper_2505_17852_amd import zo
+    rng = np.random.default_rng(14)
+    wide, _ = rand(rng, (40, 300))
+    x, y, dx = wide[:, :96], wide[:, 96:192], wide[:, 204:300]
+    want = layers.layer_norm(x.contiguous())
+    got = layers.layer_norm(x, out=y)
+    assert torch.equal(y, want[0]) and got[0] is y
+    dy = torch.ones_like(want[0])
+    grads = layers.layer_norm_backward(dy, x.contiguous(), None, *want[1:])
+    assert torch.equal(layers.layer_norm_backward(dy, x, None, *want[1:], out=dx)[0], grads[0]) and torch.equal(dx, grads[0])
+    for out in (wide[:, 1:97], wide[:, 95:191], torch.zeros(1, 96, device="cuda").expand(40, 96)):
+        with pytest.raises(zo.ZoError, match="share memory|one place"):
+            layers.layer_norm(x, out=out)

@@ -550,3 +550,31 @@ def test_one_position_at_any_distance(layers):
     wo, wfinal, mag, fmag = ref.attention(s["q"], s["k"], s["v"], s["log_decay"], s["scale"], s["initial"])
     close("o", o1, wo[:, 0], ref.unit("f32") * np.abs(wo[:, 0]) + n * 2.0 ** -24 * mag[:, 0] + 1e-37)
     close("state", state, wfinal, ref.state_bound(fmag, "f32", n))
+
+
+@pytest.mark.parametrize("order", ["heads", "time", "apart"])
+def test_outputs_between_the_inputs_values(layers, order):
+    """Outputs in the gaps of the inputs' buffer, in any order of its dimensions, are taken; on its values they are refused."""
+    from paper_2505_17852_amd import zo
+    B, T, H, D = 2, 70, 3, 40
+    s = make(np.random.default_rng(91), "f32", B, T, H, H, D, D)
+    want = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"])[0]
+    grads = layers.linear_attention_backward(s["do_d"], s["q_d"], s["k_d"], s["v_d"], s["decay_d"])
+    if order == "heads":
+        room = torch.zeros(B, T, 7 * H, D, device="cuda").view(B, T, 7, H, D).permute(2, 0, 1, 3, 4)
+    elif order == "time":
+        room = torch.zeros(T, B, H, 7, D, device="cuda").permute(3, 1, 0, 2, 4)
+    else:
+        room = torch.zeros(7, B, T, H, D, device="cuda")
+    for i, name in enumerate(("q", "k", "v")):
+        room[i].copy_(s[name + "_d"])
+    q, k, v, o = room[:4]
+    layers.linear_attention(q, k, v, s["decay_d"], out=o)
+    layers.linear_attention_backward(s["do_d"], q, k, v, s["decay_d"], dq=room[4], dk=room[5], dv=room[6])
+    assert torch.equal(o, want) and all(torch.equal(a, b) for a, b in zip(room[4:], grads))
+    assert all(torch.equal(a, s[n + "_d"]) for a, n in zip((q, k, v), "qkv"))
+    for out in (q, v, torch.zeros(D, device="cuda").expand(B, T, H, D)):
+        with pytest.raises(zo.ZoError, match="share memory|one place"):
+            layers.linear_attention(q, k, v, s["decay_d"], out=out)
+    with pytest.raises(zo.ZoError, match="dv and dk share memory"):
+        layers.linear_attention_backward(s["do_d"], q, k, v, s["decay_d"], dk=o, dv=o)
