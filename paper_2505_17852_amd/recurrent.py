@@ -155,9 +155,15 @@ class LinearLM:
 
 
 def answer(model: LinearLM, prompts: torch.Tensor, lengths: torch.Tensor | None, count: int) -> torch.Tensor:
-    """`count` tokens after each prompt [B, T] (of its own length), the likeliest one each: [B, count]."""
-    logits, states = model.forward(prompts, lengths=lengths)
+    """`count` tokens after each prompt [B, T] (of its own length, 1 .. T), the likeliest one each: [B, count]."""
     B, T = prompts.shape
+    if T < 1:
+        raise ValueError("prompts must hold a token each")
+    if lengths is not None and B:
+        shortest, longest = torch.stack(torch.aminmax(lengths)).tolist()
+        if shortest < 1 or longest > T:
+            raise ValueError(f"lengths must lie in [1, {T}], got [{shortest}, {longest}]")
+    logits, states = model.forward(prompts, lengths=lengths)
     last = torch.full((B,), T, device=prompts.device) if lengths is None else lengths.long()
     token = logits[torch.arange(B, device=prompts.device), last - 1].argmax(-1)
     out = [token]

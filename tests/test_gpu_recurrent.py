@@ -89,3 +89,16 @@ def test_a_bad_gradient_skips_the_step(rec):
     model.train_step(tokens, mask)
     for a, b in zip(keep, (model.theta, model.opt.m, model.opt.v)):
         assert torch.equal(torch.nan_to_num(a, 7.0), torch.nan_to_num(b, 7.0))
+
+
+def test_prompts_without_a_last_token_are_refused(rec):
+    """A length of 0 has no token to continue from, one past the prompts' columns no logits."""
+    model = rec.LinearLM(CFG, seed=6)
+    tokens, _ = batch(B=3, T=20)
+    good = torch.tensor([20, 1, 7], dtype=torch.int32, device="cuda")
+    assert rec.answer(model, tokens[:, :20], good, 3).shape == (3, 3)
+    for bad in ([0, 5, 20], [5, -1, 3], [5, 21, 3]):
+        with pytest.raises(ValueError, match="lengths"):
+            rec.answer(model, tokens[:, :20], torch.tensor(bad, dtype=torch.int32, device="cuda"), 3)
+    with pytest.raises(ValueError, match="prompts"):
+        rec.answer(model, tokens[:, :0], None, 3)
