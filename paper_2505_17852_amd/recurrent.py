@@ -77,14 +77,15 @@ class LinearLM:
 
     def forward(self, tokens: torch.Tensor, states=None, lengths: torch.Tensor | None = None, keep=None):
         """Logits [B, T, V] and the layers' final states for tokens [B, T]; states: the initial ones (a
-        list of the layers', or None). keep: a list that receives what backward() needs."""
+        list of the layers', or None). keep: a list that receives what the gradients need, in training (whose
+        final states nothing reads: None each)."""
         p, B, T = self.p, *tokens.shape
         h = p["emb"][tokens.long()]
         final = []
         for i in range(self.L):
             y, mean, rstd = layers.layer_norm(h, p[f"norm_w{i}"], p[f"norm_b{i}"])
             qkv = torch.matmul(y, p[f"qkv{i}"].t())
-            o, s = layers.linear_attention(*self._split(qkv), self.log_decay, lengths=lengths, return_state=True,
+            o, s = layers.linear_attention(*self._split(qkv), self.log_decay, lengths=lengths, return_state=keep is None,
                                            initial_state=None if states is None else states[i])
             final.append(s)
             if keep is not None:

@@ -102,3 +102,16 @@ def test_prompts_without_a_last_token_are_refused(rec):
             rec.answer(model, tokens[:, :20], torch.tensor(bad, dtype=torch.int32, device="cuda"), 3)
     with pytest.raises(ValueError, match="prompts"):
         rec.answer(model, tokens[:, :0], None, 3)
+
+
+def test_training_asks_for_no_final_states(rec, monkeypatch):
+    """Nothing reads them there; a prompt's are wanted."""
+    asked = []
+    whole = rec.layers.linear_attention
+    monkeypatch.setattr(rec.layers, "linear_attention", lambda *a, **kw: asked.append(kw["return_state"]) or whole(*a, **kw))
+    model = rec.LinearLM(CFG, seed=7)
+    tokens, mask = batch()
+    model.loss_and_gradients(tokens, mask)
+    assert asked == [False] * CFG["n_layers"]
+    _, states = model.forward(tokens)
+    assert asked[CFG["n_layers"]:] == [True] * CFG["n_layers"] and all(s.dim() == 4 for s in states)
