@@ -29,6 +29,7 @@ import torch
 from . import layers
 
 HEAD_DIM = 64  # of keys and values, or the hidden size where that is smaller
+HEAD_VALUES = 1 << 27  # logits in memory at a time, in training (those of the large model's batch would take 26 GB in bf16)
 
 
 class LinearLM:
@@ -77,15 +78,19 @@ class LinearLM:
 
     def forward(self, tokens: torch.Tensor, states=None, lengths: torch.Tensor | None = None, keep=None):
         """Logits [B, T, V] and the layers' final states for tokens [B, T]; states: the initial ones (a
-        list of the layers', or None). keep: a list that receives what the gradients need, in training (whose
-        final states nothing reads: None each)."""
+        list of the layers', or None). keep: a list that receives what the gradients need."""
+        y, final = self._hidden(tokens, states, lengths, keep)
+        return torch.matmul(y, self.p["head"].t()) + self.p["head_b"], final
+
+    def _hidden(self, tokens, states=None, lengths=None, keep=None, return_states=True):
+        """What the logits are formed from [B, T, H], and the final states (None each where they are not wanted)."""
         p, B, T = self.p, *tokens.shape
         h = p["emb"][tokens.long()]
         final = []
         for i in range(self.L):
             y, mean, rstd = layers.layer_norm(h, p[f"norm_w{i}"], p[f"norm_b{i}"])
             qkv = torch.matmul(y, p[f"qkv{i}"].t())
-            o, s = layers.linear_attention(*self._split(qkv), self.log_decay, lengths=lengths, return_state=keep is None,
+            o, s = layers.linear_attention(*self._split(qkv), self.log_decay, lengths=lengths, return_state=return_states,
                                            initial_state=None if states is None else states[i])
             final.append(s)
             if keep is not None:
@@ -94,7 +99,7 @@ class LinearLM:
         y, mean, rstd = layers.layer_norm(h, p["norm_w"], p["norm_b"])
         if keep is not None:
             keep.append((h, y, mean, rstd))
-        return torch.matmul(y, p["head"].t()) + p["head_b"], final
+        return y, final
 
     def loss_and_gradients(self, tokens: torch.Tensor, mask: torch.Tensor | None):
         """The masked mean cross-entropy of the next tokens (tokens [B, T + 1]), a device scalar, and the
@@ -102,20 +107,24 @@ class LinearLM:
         p, inputs, targets = self.p, tokens[:, :-1], tokens[:, 1:].long()
         B, T = inputs.shape
         keep = []
-        logits, _ = self.forward(inputs, keep=keep)
+        y = self._hidden(inputs, keep=keep, return_states=False)[0].view(B * T, self.H)
         weight = torch.ones(B, T, device=tokens.device) if mask is None else mask.float()
-        weight = weight / weight.sum().clamp(min=1.0)
-        logp = torch.log_softmax(logits.float(), -1)
-        loss = -(logp.gather(2, targets.unsqueeze(2)).squeeze(2) * weight).sum()
-        dlogits = torch.exp(logp)
-        dlogits.scatter_add_(2, targets.unsqueeze(2), -torch.ones_like(targets, dtype=torch.float32).unsqueeze(2))
-        dlogits = (dlogits * weight.unsqueeze(2)).to(self.theta.dtype).view(B * T, self.V)
-        g = {}
-        h, y, mean, rstd = keep.pop()
-        g["head"] = torch.matmul(dlogits.t(), y.view(B * T, self.H))
-        g["head_b"] = dlogits.float().sum(0)
-        dh, g["norm_w"], g["norm_b"] = layers.layer_norm_backward(
-            torch.matmul(dlogits, p["head"]).view(B, T, self.H), h, p["norm_w"], mean, rstd)
+        weight = (weight / weight.sum().clamp(min=1.0)).view(-1, 1)
+        targets = targets.reshape(-1, 1)
+        loss, dy, g = torch.zeros((), device=tokens.device), torch.empty_like(y), {"head": None, "head_b": None}
+        rows = max(1, HEAD_VALUES // self.V)
+        for at in range(0, max(B * T, 1), rows):
+            part = slice(at, at + rows)
+            logp = torch.log_softmax((torch.matmul(y[part], p["head"].t()) + p["head_b"]).float(), -1)
+            loss = loss - (logp.gather(1, targets[part]) * weight[part]).sum()
+            dlogits = logp.exp_()
+            dlogits.scatter_add_(1, targets[part], -torch.ones_like(targets[part], dtype=torch.float32))
+            dlogits = dlogits.mul_(weight[part]).to(self.theta.dtype)
+            torch.matmul(dlogits, p["head"], out=dy[part])
+            for name, x in (("head", torch.matmul(dlogits.t(), y[part])), ("head_b", dlogits.float().sum(0))):
+                g[name] = x if g[name] is None else g[name].float().add_(x)  # parts are added in fp32
+        h, _, mean, rstd = keep.pop()
+        dh, g["norm_w"], g["norm_b"] = layers.layer_norm_backward(dy.view(B, T, self.H), h, p["norm_w"], mean, rstd)
         for i in reversed(range(self.L)):
             h, y, mean, rstd, qkv, o = keep.pop()
             flat = dh.view(B * T, self.H)

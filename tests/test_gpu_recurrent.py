@@ -115,3 +115,33 @@ def test_training_asks_for_no_final_states(rec, monkeypatch):
     assert asked == [False] * CFG["n_layers"]
     _, states = model.forward(tokens)
     assert asked[CFG["n_layers"]:] == [True] * CFG["n_layers"] and all(s.dim() == 4 for s in states)
+
+
+def test_the_head_by_parts_is_the_head(rec, monkeypatch):
+    """Logits of 37 positions at a time against all 280 at once (fp32): the same sums in another order. A loss or gradient
+    is a sum of at most 280 such terms, each through fp32 sums of at most 280 + 128 + 50 values: 1,000 units."""
+    model = rec.LinearLM(CFG, seed=8)
+    tokens, mask = batch()
+    want, wgrads = model.loss_and_gradients(tokens, mask)
+    monkeypatch.setattr(rec, "HEAD_VALUES", 37 * CFG["vocab"] + 3)
+    got, grads = model.loss_and_gradients(tokens, mask)
+    unit = 1000 * 2.0 ** -24
+    assert abs(float(got) - float(want)) <= unit * abs(float(want))
+    for name, a, b in zip(model.p, grads, wgrads):
+        assert a.dtype == torch.float32 and a.shape == b.shape
+        assert float((a - b).norm()) <= 8 * unit * float(b.norm()), name
+
+
+def test_the_head_s_memory_is_bounded(rec):
+    """16,384 positions of 50,000 logits: 3.3 GB each time they are held in fp32. A part holds at most HEAD_VALUES of them,
+    six times over at its peak; the rest of the model and its gradients is under 0.5 GB."""
+    model = rec.LinearLM(dict(n_layers=1, vocab=50_000, embed=64, hidden=64, wdtype=0), seed=9)
+    tokens, _ = batch(B=16, T=1024, V=50_000)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    loss, _ = model.loss_and_gradients(tokens, None)
+    assert np.isfinite(float(loss))
+    peak = torch.cuda.max_memory_allocated() - before
+    print(f"{peak / 2 ** 30:.2f} GiB", flush=True)
+    assert peak <= 6 * 4 * (1 << 27) + (1 << 29)
