@@ -5,7 +5,9 @@ Argument marshalling only: every computation runs in the library's HIP
 kernels, on the current torch stream unless one is passed (which then serves as the
 current one: the caller makes it wait for what it needs). Outputs and
 workspaces are allocated by torch, for the call's stream, when they are not given. Errors: ValueError
-for arguments that do not fit together, zo.ZoError for what the library refuses.
+for arguments that do not fit together, zo.ZoError for what the library refuses. torch's autograd does not see
+the calls: inputs that require gradients are taken under torch.no_grad() only (ValueError otherwise), and gradients
+are those of the backward functions.
 
     layer_norm, layer_norm_backward
     linear_attention, linear_attention_backward, linear_attention_step
@@ -94,6 +96,15 @@ def _device(t: torch.Tensor, name: str, dtype=None, like: torch.Tensor | None = 
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if like is not None and t.get_device() != like.get_device():
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+
+
+_recording = torch.is_grad_enabled
+
+
+def _refuse_gradients():
+    """For a call whose inputs require gradients while torch records: its outputs would silently carry none."""
+    raise ValueError("inputs that require gradients: torch's autograd does not see the layers' calls; call them under "
+                     "torch.no_grad() and their backward functions for the gradients")
 
 
 def _flat(t: torch.Tensor | None, name: str, dtype, shape, like: torch.Tensor):
@@ -203,6 +214,9 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
                        final_state, workspace)
     L = lib()
     B, T, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 4, scale)
+    if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad
+                         or (initial_state is not None and initial_state.requires_grad)):
+        _refuse_gradients()
     states = (B, Hkv, Dk, Dv)
     o, ho = _new_heads(q, B, T, Hq, Dv) if out is None else (out, _heads(out, "out", (B, T, Hq, Dv), q))
     f32 = torch.float32
@@ -263,6 +277,8 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
         return _beside(stream, linear_attention_step, q, k, v, log_decay, state, scale, slots, out)
     L = lib()
     B, _, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 3, scale)
+    if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad or state.requires_grad):
+        _refuse_gradients()
     n = state.shape[0]
     if n > 0x7fffffff:
         raise ValueError("state must hold fewer than 2^31 states")
@@ -313,6 +329,9 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     L = lib()
     rows, D, xs = _rows(x, "x")
     wtype, w, b = _norm_params(weight, bias, D, x)
+    if _recording() and (x.requires_grad or (weight is not None and weight.requires_grad)
+                         or (bias is not None and bias.requires_grad)):
+        _refuse_gradients()
     dev = x.device
     y = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
     ys = D if out is None else _rows(y, "out", x.shape, x)[2]

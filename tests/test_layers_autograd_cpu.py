@@ -1,0 +1,44 @@
+"""The layers and torch's autograd, on the host: nothing is silently cut off from a gradient."""
+import pytest
+import torch
+
+import layers_fake as fake
+
+
+@pytest.fixture
+def device(monkeypatch):
+    from paper_2505_17852_amd import layers
+    dev = fake.Device(layers, monkeypatch)
+    dev.layers = layers
+    return dev
+
+
+def calls(m):
+    q = lambda: torch.ones(2, 5, 2, 8)  # noqa: E731
+    row = lambda: torch.ones(2, 2, 8)  # noqa: E731
+    decay = torch.zeros(2)
+    return {
+        "linear_attention": (lambda a: m.linear_attention(a[0], a[1], a[2], decay, initial_state=a[3]),
+                             [q(), q(), q(), torch.zeros(2, 2, 8, 8)]),
+        "linear_attention_step": (lambda a: m.linear_attention_step(a[0], a[1], a[2], decay, a[3]),
+                                  [row(), row(), row(), torch.zeros(2, 2, 8, 8)]),
+        "layer_norm": (lambda a: m.layer_norm(*a), [torch.ones(3, 8), torch.ones(8), torch.ones(8)]),
+    }
+
+
+@pytest.mark.parametrize("name", ["linear_attention", "linear_attention_step", "layer_norm"])
+def test_inputs_that_require_gradients_are_refused_where_they_would_be_recorded(device, name):
+    f, args = calls(device.layers)[name]
+    f(args)
+    before = len(device.library.calls)
+    for i in range(len(args)):
+        args[i].requires_grad_(True)
+        with pytest.raises(ValueError, match="no_grad"):
+            f(args)
+        assert len(device.library.calls) == before
+        with torch.no_grad():
+            f(args)
+        with torch.inference_mode():
+            f(args)
+        args[i].requires_grad_(False)
+        before = len(device.library.calls)
