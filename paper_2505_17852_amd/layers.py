@@ -423,6 +423,7 @@ class AdamW:
         else:
             self._m = torch.zeros(at, dtype=torch.float32, device=dev)
             self._v = torch.zeros(at, dtype=torch.float32, device=dev)
+        self._leaves = [p for p in self.params if p.requires_grad]
         self._shapes = [p.shape for p in self.params]
         self._dtypes = [p.dtype for p in self.params]
         self._devices = [first.get_device()] * len(self.params)
@@ -472,6 +473,8 @@ class AdamW:
                               self._v_scale.data_ptr() if eight else None,
                               gs, sk, _stream(like)))
         self.step_count += 1
+        if self._leaves:  # what torch has recorded on them is about the values before
+            torch.autograd.graph.increment_version(self._leaves)
 
     def moments(self, stream=None):
         """The flat fp32 (m, v): the buffers themselves (32 bits), or the values that the codes stand for."""

@@ -257,3 +257,16 @@ def test_second_moments_and_denominators_below_the_normal_range(layers, eps, bit
     change = LR * np.abs(ge) / np.maximum(np.sqrt(ge ** 2) + e, 1e-300)
     bound = np.maximum(change - lo, hi - change) + ref.ulps(8) * change + ref.ulps(2)
     within("p", host(p), 1.0 - np.sign(ge) * change, bound)
+
+
+def test_parameters_that_require_gradients(layers):
+    """The values of a step on tensors that require none, and the change is known to torch."""
+    rng = np.random.default_rng(15)
+    p0, g = rand(rng, 500), rand(rng, 500)
+    p, w = p0.clone(), p0.clone().requires_grad_(True)
+    layers.AdamW([p], lr=LR).step([g])
+    held = (w * w).sum()
+    layers.AdamW([w], lr=LR).step([g])
+    assert torch.equal(w.detach(), p)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        held.backward()

@@ -42,3 +42,16 @@ def test_inputs_that_require_gradients_are_refused_where_they_would_be_recorded(
             f(args)
         args[i].requires_grad_(False)
         before = len(device.library.calls)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_counts_as_a_change_of_its_parameters(device, bits):
+    """A gradient whose backward pass needs the values from before the step fails in torch, as after torch's own optimizers."""
+    w = torch.ones(4, requires_grad=True)
+    opt = device.layers.AdamW([w], state_bits=bits)
+    loss = (w * w).sum()
+    opt.step([torch.ones(4)])
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    (w * w).sum().backward()
+    assert torch.equal(w.grad, torch.full((4,), 2.0))
