@@ -908,18 +908,20 @@ hipError_t launch_chunks(const LinCall& c, Plan pl, hipStream_t st) {
     members += p.heads * ((p.dz + SL - 1) / SL);
     most = std::max(most, p.dx * p.dz);
   }
-  if (pl.segments > 1) {
-    pl.groups = states * (pl.segments - 1);
-    pl.members = slices;
-    linattn_chunk_kernel<T, DX, SL, even, true><<<grid(pl.groups, slices), kThreads, 0, st>>>(c, pl);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (pl.segments > 2) {
-      dim3 g = wide_grid(states * ((most + kThreads - 1) / kThreads));
-      g.z = c.npasses;
-      linattn_scan_kernel<<<g, kThreads, 0, st>>>(c, pl);
-      e = hipGetLastError();
+  if constexpr (SL == 64) {  // (slices of 128 come with 256 workgroups and more, and those in one segment)
+    if (pl.segments > 1) {
+      pl.groups = states * (pl.segments - 1);
+      pl.members = slices;
+      linattn_chunk_kernel<T, DX, SL, even, true><<<grid(pl.groups, slices), kThreads, 0, st>>>(c, pl);
+      hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
+      if (pl.segments > 2) {
+        dim3 g = wide_grid(states * ((most + kThreads - 1) / kThreads));
+        g.z = c.npasses;
+        linattn_scan_kernel<<<g, kThreads, 0, st>>>(c, pl);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+      }
     }
   }
   pl.groups = states * pl.segments;

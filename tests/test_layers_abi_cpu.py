@@ -207,3 +207,15 @@ def test_states_that_share_memory_in_part_are_refused(layers):
         st = layers.lib().zo_linear_attention_backward(s, h, h, h, h, h, h, h, FAKE, None, None, a, b, FAKE, 1 << 40,
                                                        None)
         assert st == -1 and "different" in error()
+
+
+def test_no_kernel_that_no_call_reaches(layers):
+    """Slices of 128 columns have 256 workgroups and more, which are never split into segments: no kernel for both."""
+    from paper_2505_17852_amd import zo
+    nm = shutil.which("nm")
+    if nm is None:
+        pytest.skip("no nm")
+    names = subprocess.run([nm, "-C", zo.LIB_PATH], check=True, capture_output=True, text=True).stdout
+    chunks = set(re.findall(r"linattn_chunk_kernel<([^>]*)>", names))
+    assert any(x.endswith("128, 128, true, false") for x in chunks)
+    assert not [x for x in chunks if x.endswith(("128, 128, true, true", "128, 128, false, true"))]
