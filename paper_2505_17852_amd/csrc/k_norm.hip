@@ -275,13 +275,13 @@ __global__ __launch_bounds__(threads_of<TPR>()) void norm_backward_kernel(NormAr
 __global__ __launch_bounds__(1024) void norm_sums_kernel(const float* partial, int parts, int64_t D, float* dw,
                                                          float* db) {
   __shared__ float join[16][64];
-  float* out = blockIdx.y ? db : dw;
+  float* out = blockIdx.z ? db : dw;
   if (!out) return;
   const int c = threadIdx.x & 63, share = threadIdx.x >> 6;
-  const int64_t j = (int64_t)blockIdx.x * 64 + c;
+  const int64_t j = block_id() * 64 + c;
   float s = 0;
   if (j < D) {
-    const float* p = partial + blockIdx.y * D + j;
+    const float* p = partial + blockIdx.z * D + j;
 #pragma unroll 8
     for (int k = share; k < parts; k += 16) s += p[(int64_t)k * 2 * D];
   }
@@ -411,8 +411,11 @@ hipError_t backward(const NormArgs& a, hipStream_t s) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.dw || a.db)
-    norm_sums_kernel<<<dim3((unsigned)((a.D + 63) / 64), 2), 1024, 0, s>>>(a.partial, parts, a.D, a.dw, a.db);
+  if (a.dw || a.db) {
+    dim3 grid = wide_grid((a.D + 63) / 64);  // (rows of 2^28 values and more: 2^32 threads)
+    grid.z = 2;
+    norm_sums_kernel<<<grid, 1024, 0, s>>>(a.partial, parts, a.D, a.dw, a.db);
+  }
   return hipGetLastError();
 }
 

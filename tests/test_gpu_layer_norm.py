@@ -218,3 +218,16 @@ def test_rows_between_the_input_s_rows(layers):
     for out in (wide[:, 1:97], wide[:, 95:191], torch.zeros(1, 96, device="cuda").expand(40, 96)):
         with pytest.raises(zo.ZoError, match="share memory|one place"):
             layers.layer_norm(x, out=out)
+
+
+def test_a_row_past_the_threads_of_one_grid_dimension(layers):
+    """One row of 2^28 + 65 values: the column sums (of one row) are dy xhat and dy, all of them, xhat by the mean and rstd
+    that the call keeps. Here and in torch's, three roundings each of values up to 6.5 |dy|: 6 x 6.5 x 2^-24 |dy|."""
+    D = (1 << 28) + 65
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(1, D, generator=gen, device="cuda", dtype=torch.bfloat16)
+    dy = torch.randn(1, D, generator=gen, device="cuda", dtype=torch.bfloat16)
+    _, mean, rstd = layers.layer_norm(x)
+    _, dw, db = layers.layer_norm_backward(dy, x, None, mean, rstd)
+    assert torch.equal(db, dy[0].float())
+    assert float(((dw - dy[0].float() * ((x[0].float() - mean) * rstd)).abs() / dy[0].float().abs().clamp(min=1e-3)).max()) <= 39 * 2.0 ** -24
