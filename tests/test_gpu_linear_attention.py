@@ -578,3 +578,99 @@ def test_outputs_between_the_inputs_values(layers, order):
             layers.linear_attention(q, k, v, s["decay_d"], out=out)
     with pytest.raises(zo.ZoError, match="dv and dk share memory"):
         layers.linear_attention_backward(s["do_d"], q, k, v, s["decay_d"], dk=o, dv=o)
+
+
+# B, T, Hq, Hkv, Dk, Dv, lengths: up to four positions (times the query heads of a state: up to 4, up to 16, and past it)
+FEW = {
+    "two": (3, 2, 2, 2, 53, 61, None),
+    "three": (4, 3, 3, 3, 128, 96, [0, 1, 3, 2]),
+    "four": (5, 4, 2, 2, 64, 64, [4, 0, 1, 3, 2]),
+    "four_wide": (2, 4, 1, 1, 256, 200, [3, 4]),
+    "one_shared": (3, 1, 8, 2, 96, 128, [1, 0, 1]),
+    "two_shared": (3, 2, 8, 1, 33, 130, [2, 1, 0]),
+    "three_shared": (2, 3, 8, 2, 200, 40, None),
+    "four_shared": (4, 4, 8, 2, 64, 120, [0, 1, 3, 4]),
+    "four_shared_past": (4, 4, 10, 2, 64, 120, [0, 1, 3, 4]),
+    "two_shared_past": (2, 2, 9, 1, 40, 256, [2, 1]),
+}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("state", [False, True])
+@pytest.mark.parametrize("name", list(FEW))
+def test_few_positions(layers, name, state, dtype):
+    """With and without states, lengths inside, heads that share, odd sizes."""
+    B, T, Hq, Hkv, Dk, Dv, lengths = FEW[name]
+    s = make(np.random.default_rng(len(name) + 5 * state), dtype, B, T, Hq, Hkv, Dk, Dv, state, lengths)
+    o, final = check_forward(layers, s)
+    grads = check_backward(layers, s)
+    _near_fp32(layers, s) if dtype == "bf16" else None
+    for b, n in enumerate(lengths or []):
+        assert not o[b, n:].any() and not any(g[b, n:].any() for g in grads[:3])
+        if n == 0 and state:
+            assert torch.equal(final[b], s["initial_d"][b]) and torch.equal(grads[3][b], s["dfinal_d"][b])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 3, 4])
+def test_decays_at_their_ends_over_few_positions(layers, T, dtype):
+    decay = np.array([0.0, -np.inf, -3.0, -40.0], dtype=np.float32)
+    s = make(np.random.default_rng(T), dtype, 2, T, 8, 4, 40, 24, True, [T, T - 1], decay)
+    check_forward(layers, s)
+    check_backward(layers, s)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("at", [0, 1, 3])
+def test_a_bad_value_among_few_positions(layers, at, bad):
+    """As over many: outputs from its position on only, gradients of k and v up to it only; past a length it is not read."""
+    s = make(np.random.default_rng(17), "bf16", 2, 4, 2, 2, 64, 64, False, [4, at])
+    args = dict(scale=s["scale"], lengths=s["lengths_d"])
+    base, _ = layers.linear_attention(s["q_d"], s["k_d"], s["v_d"], s["decay_d"], **args)
+    grads = layers.linear_attention_backward(s["do_d"], s["q_d"], s["k_d"], s["v_d"], s["decay_d"], **args)
+    for name in ("q", "k", "v", "do"):
+        x = {n: s[n + "_d"].clone() for n in ("q", "k", "v", "do")}
+        x[name][:, at, 0, 5] = bad
+        o, _ = layers.linear_attention(x["q"], x["k"], x["v"], s["decay_d"], **args)
+        got = layers.linear_attention_backward(x["do"], x["q"], x["k"], x["v"], s["decay_d"], **args)
+        for a, w in zip((o, *got[:3]), (base, *grads[:3])):
+            assert torch.equal(a[1], w[1]) and torch.equal(a[0, :, 1], w[0, :, 1]), name
+        if name != "do":
+            assert torch.equal(o[0, :at], base[0, :at]) and not torch.isfinite(o[0, at, 0]).all(), name
+        if name in ("q", "do"):
+            assert all(torch.equal(a[0, at + 1:], w[0, at + 1:]) for a, w in zip(got[1:3], grads[1:3])), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_segments(layers, dtype):
+    """One sequence of 5,000 positions in 19 segments, and one that ends within them."""
+    s = make(np.random.default_rng(27), dtype, 1, 5000, 1, 1, 64, 64, True)
+    check_forward(layers, s)
+    check_backward(layers, s)
+    s["lengths"], s["lengths_d"] = [3333], torch.tensor([3333], dtype=torch.int32, device="cuda")
+    check_forward(layers, s)
+    check_backward(layers, s)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,D", [(64, 64), (50, 64), (100, 128), (190, 200)])
+def test_states_are_as_exact_as_their_factors(layers, T, D, dtype):
+    """Keys and queries of one 1 each, at a row of its own: every value of a final state (or an initial one's gradient) is one
+    value times a power of gamma. Within its chunk that is two powers (each: an exponent under 1 rounded to 2^-23, the power
+    to 2^-23), two products, and the value in parts, 2^-24 left out: 5 of 2^-23; 3 more for each chunk after it."""
+    H = 3
+    s = make(np.random.default_rng(T + D), dtype, 2, T, H, H, D, D, False, None, ref.log_decays(H, 8.0, 11.0))
+    hot = torch.zeros(T, D, device="cuda", dtype=s["q_d"].dtype)
+    hot[torch.arange(T), torch.arange(T)] = 1.0
+    hot = hot.view(1, T, 1, D).expand(2, T, H, D).contiguous()
+    unit = (5 + 3 * ((T - 1) // 64)) * 2.0 ** -23
+    ld = s["log_decay"].astype(np.float64)[None, :, None, None]
+    _, final = layers.linear_attention(hot, hot, s["v_d"], s["decay_d"], scale=1.0, return_state=True)
+    left = T - 1 - np.arange(T)
+    want = s["v"].astype(np.float64).transpose(0, 2, 1, 3) * np.exp(ld * left[None, None, :, None])
+    close("final", final[:, :, :T], want, unit * np.abs(want) + 1e-37)
+    assert not final[:, :, T:].any()
+    got = layers.linear_attention_backward(s["do_d"], hot, hot, s["v_d"], s["decay_d"], scale=1.0, return_dinitial=True)[3]
+    want = s["do"].astype(np.float64).transpose(0, 2, 1, 3) * np.exp(ld * (np.arange(T) + 1)[None, None, :, None])
+    close("dinitial", got[:, :, :T], want, unit * np.abs(want) + 1e-37)
+    assert not got[:, :, T:].any()
