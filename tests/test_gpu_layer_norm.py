@@ -231,3 +231,40 @@ def test_a_row_past_the_threads_of_one_grid_dimension(layers):
     _, dw, db = layers.layer_norm_backward(dy, x, None, mean, rstd)
     assert torch.equal(db, dy[0].float())
     assert float(((dw - dy[0].float() * ((x[0].float() - mean) * rstd)).abs() / dy[0].float().abs().clamp(min=1e-3)).max()) <= 39 * 2.0 ** -24
+
+
+MANY_ROWS = [(1300, 1025), (2100, 2048), (1100, 8192), (600, 9000), (2500, 4096)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,D", MANY_ROWS)
+def test_several_rows_for_each_workgroup(layers, rows, D, dtype):
+    """More rows than workgroups where several waves share one."""
+    check(layers, np.random.default_rng(rows), rows, D, dtype, "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,D", MANY_ROWS)
+def test_several_rows_in_place_between_gaps(layers, rows, D, dtype):
+    """dx in place of dy and of x, y in place of x: the same bits as apart, and no other value of the buffer changes."""
+    rng = np.random.default_rng(D)
+    wide, _ = rand(rng, (rows, 2 * D + 5), dtype)
+    w, _ = rand(rng, D, dtype, 0.2, 1.0)
+    at = {"x": slice(1, D + 1), "dy": slice(D + 3, 2 * D + 3)}
+    x, dy = (wide[:, at[n]].contiguous() for n in ("x", "dy"))
+    y, mean, rstd = layers.layer_norm(x, w)
+    grads = layers.layer_norm_backward(dy, x, w, mean, rstd)
+
+    def others(buffer, name):
+        kept = torch.ones(buffer.shape[1], dtype=torch.bool, device="cuda")
+        kept[at[name]] = False
+        return torch.equal(buffer[:, kept], wide[:, kept])
+
+    for name in ("dy", "x"):
+        held = wide.clone()
+        got = layers.layer_norm_backward(held[:, at["dy"]], held[:, at["x"]], w, mean, rstd, out=held[:, at[name]])
+        assert all(torch.equal(a, b) for a, b in zip(got, grads)) and others(held, name)
+        assert torch.equal(held[:, at[name]], grads[0])
+    held = wide.clone()
+    layers.layer_norm(held[:, at["x"]], w, out=held[:, at["x"]])
+    assert torch.equal(held[:, at["x"]], y) and others(held, "x")
