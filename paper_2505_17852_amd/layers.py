@@ -22,6 +22,7 @@ from operator import attrgetter
 import torch
 
 from . import zo
+from .zo import _beside, _record
 
 MAX_DIM = 256   # ZO_LINATTN_MAX_DIM
 BLOCK = 256     # ZO_ADAMW_BLOCK
@@ -118,26 +119,6 @@ def _flat(t: torch.Tensor | None, name: str, dtype, shape, like: torch.Tensor):
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
-
-
-def _record(stream, values):
-    for x in values:
-        if isinstance(x, torch.Tensor):
-            x.record_stream(stream)
-        elif isinstance(x, (list, tuple)):
-            _record(stream, x)
-
-
-def _beside(stream, call, *args):
-    """call(*args) on another stream than the current one. What it allocates is allocated there: a block that was
-    freed on the current stream may still be in use by work queued on that. The tensors that it is given are held
-    until `stream` has done with them, those that it returns until the current stream has."""
-    here = torch.cuda.current_stream(stream.device)
-    with torch.cuda.stream(stream):
-        out = call(*args)
-    _record(stream, args)
-    _record(here, out if isinstance(out, tuple) else (out,))
-    return out
 
 
 # ---- linear attention ----

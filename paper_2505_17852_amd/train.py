@@ -57,13 +57,13 @@ def train(cfg, theta: torch.Tensor, tokens: torch.Tensor, mask: torch.Tensor | N
     fd = estimator == "fd"
     B, C1 = tokens.shape
     dev = theta.device
-    ws = zo.new_workspace(cfg, N, B, C1 - 1, device=dev)
-    L1 = torch.empty(N, dtype=torch.float32, device=dev)
-    L2 = torch.empty(1 if fd else N, dtype=torch.float32, device=dev)
-    hist = torch.empty(steps, dtype=torch.float32, device=dev)
-    # the loss bookkeeping runs on the same stream as the library calls
+    # buffers and loss bookkeeping are on the same stream as the library calls
     ctx = torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
     with ctx:
+        ws = zo.new_workspace(cfg, N, B, C1 - 1, device=dev)
+        L1 = torch.empty(N, dtype=torch.float32, device=dev)
+        L2 = torch.empty(1 if fd else N, dtype=torch.float32, device=dev)
+        hist = torch.empty(steps, dtype=torch.float32, device=dev)
         for k in range(steps):
             tok, msk = (tokens, mask) if batches is None or k == 0 else batches(k)
             check = k == 0 or batches is not None

@@ -112,6 +112,26 @@ def _stream(stream):
     return C.c_void_p(stream.cuda_stream)
 
 
+def _record(stream, values):
+    for x in values:
+        if isinstance(x, torch.Tensor):
+            x.record_stream(stream)
+        elif isinstance(x, (list, tuple)):
+            _record(stream, x)
+
+
+def _beside(stream, call, *args):
+    """call(*args) on another stream than the current one. What it allocates is allocated there: a block that was
+    freed on the current stream may still be in use by work queued on that. The tensors that it is given are held
+    until `stream` has done with them, those that it returns until the current stream has."""
+    here = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    _record(stream, args)
+    _record(here, out if isinstance(out, tuple) else (out,))
+    return out
+
+
 def _dev(t: torch.Tensor, dtype, name: str):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
@@ -180,6 +200,9 @@ def perturbed_losses(cfg, theta: torch.Tensor, seed: int, eps: float, N: int,
     check_tokens (default) this wrapper rejects them first (one device
     sync). products: PRODUCTS_AUTO (zo_perturbed_losses), or PRODUCTS_FUSED /
     PRODUCTS_SPLIT (zo_perturbed_losses_ex, for measurement)."""
+    if stream is not None and (Lplus is None or Lminus is None or workspace is None):
+        return _beside(stream, perturbed_losses, cfg, theta, seed, eps, N, tokens, mask, i0, Lplus, Lminus, workspace,
+                       None, check_tokens, products)
     c = _cfg(cfg)
     if tokens.dim() != 2:
         raise ValueError("tokens must be [B][C+1]")
@@ -293,6 +316,9 @@ def fd_losses(cfg, theta: torch.Tensor, seed: int, eps: float, N: int, tokens: t
     """Forward differences: returns (L [N], L0 [1]) as device fp32 tensors
     (asynchronous): the losses at theta + eps z_n and at theta. products as
     for perturbed_losses (zo_fd_losses_ex when not PRODUCTS_AUTO)."""
+    if stream is not None and (L is None or L0 is None or workspace is None):
+        return _beside(stream, fd_losses, cfg, theta, seed, eps, N, tokens, mask, i0, L, L0, workspace, None, check_tokens,
+                       products)
     c = _cfg(cfg)
     if tokens.dim() != 2:
         raise ValueError("tokens must be [B][C+1]")
@@ -341,12 +367,16 @@ def fd_update(cfg, theta: torch.Tensor, seed: int, eps: float, lr: float, L: tor
 
 
 def debug_probe(kind: int, seed: int, i: int, j0: int, n: int, device="cuda", stream=None):
+    if stream is not None:
+        return _beside(stream, debug_probe, kind, seed, i, j0, n, device)
     out = torch.empty(n, dtype=torch.float32, device=device)
     _check(lib().zo_debug_probe(kind, seed, i, j0, n, _dev(out, torch.float32, "out"), _stream(stream)))
     return out
 
 
 def debug_gauss_pairs(words: torch.Tensor, stream=None) -> torch.Tensor:
+    if stream is not None:
+        return _beside(stream, debug_gauss_pairs, words)
     if words.numel() % 2:
         raise ValueError("words must hold whole pairs")
     out = torch.empty(words.numel(), dtype=torch.float32, device=words.device)
