@@ -147,7 +147,8 @@ int zo_layer_norm_backward(int32_t xdtype, int32_t wdtype, int64_t rows, int64_t
  * The moments of all tensors lie in flat arrays; a tensor's begin at its
  * state_offset, a multiple of ZO_ADAMW_BLOCK, and take whole blocks. All tensors are updated
  * at once: the parameters of two, or their moments, may not overlap (ZO_EINVAL; a tied
- * tensor is given once, with the sum of its gradients).
+ * tensor is given once, with the sum of its gradients). A gradient may be shared by tensors, but lies in
+ * no parameter.
  *   32 bits  m and v fp32
  *   8 bits   m int8 and v uint8 codes, and m_scale and v_scale fp32, the largest |m| and v of each
  *            block: a code c stands for m_scale sign(c) (c / 127)^2, or v_scale (c / 255)^4.
@@ -176,10 +177,15 @@ typedef struct {
  *   m, v             device moments; m_scale, v_scale: 8 bits only (NULL otherwise)
  *   grad_scale       device fp32 [1] or NULL (1): a clipping or unscaling factor. If it
  *                    is not finite the step is skipped on the device: parameters and
- *                    moments stay bit for bit as they are
+ *                    moments stay bit for bit as they are. Bias corrections go by cfg->step alone:
+ *                    a caller that counts a skipped step corrects for an update that no moment holds
+ *                    (a first step skipped makes the next one's change 0.74 of what it would be, at
+ *                    betas of 0.9 and 0.999), one that does not, by skipped_out, has the formula's
  *   skipped_out      device int32 [1] or NULL: 1 if it was skipped, else 0
  * Parameters of 32-bit and 16-bit types may be mixed, and aligned as their type needs.
- * cfg is read by the call: a captured launch replays with its step's lr and bias corrections. */
+ * A parameter is rounded once, to nearest: in bf16 a change under 2^-9 of the value is lost, step after
+ * step (a weight decay of 0.1 at an lr of 1e-3 alone changes nothing). Where small changes count, keep fp32
+ * parameters and cast them. cfg is read by the call: a captured launch replays with its step's lr and bias corrections. */
 int zo_adamw(const zo_adamw_config* cfg, const zo_adamw_tensor* tensors, int32_t n_tensors, void* m, void* v,
              float* m_scale, float* v_scale, const float* grad_scale, int32_t* skipped_out, void* stream);
 

@@ -15,9 +15,11 @@
 // near a rounding boundary depends on the last bit of the moment, so moments and
 // codes are those of the definition's operations, one IEEE rounding each, without
 // contraction. Roots and quotients of that kind take ten instructions and
-// more; a code is first found from the hardware's approximate ones (a few units in the last
-// place off) and worked out again only where it lies within 2^-11 of a boundary,
-// which their error cannot reach across (128 million parameters: 0.53 -> 0.31 to 0.34 ms, 4 TB/s; decoding the
+// more; a code is first found from the hardware's approximate ones and worked out again only where it lies
+// within 2^-11 of a boundary, which their error cannot reach across: 1 / top is within 2^-22 (a subnormal one; 2^-24
+// otherwise), products within 2^-24, a root within 2^-23 and half of what lies under it, so that a code is known to
+// 2^-21 relative, the definition's own operations to 2^-22, together at most 255 x 2^-20 = 2^-12 apart
+// (128 million parameters: 0.53 -> 0.31 to 0.34 ms, 4 TB/s; decoding the
 // moments for the caller 0.20 ms, 6.3 TB/s).
 #include <hip/hip_runtime.h>
 
@@ -98,7 +100,7 @@ __device__ __forceinline__ float decode_v(int c, float top) {
 }
 constexpr float kNear = 0x1p-11f;
 
-// Whether the nearest whole number of t, at most 255 and known to 2^-18 relative, is certain (not of a NaN).
+// Whether the nearest whole number of t, at most 255 and known to 2^-20 relative, is certain (not of a NaN).
 __device__ __forceinline__ bool certain(float t) { return fabsf(t - rintf(t)) < 0.5f - kNear; }
 
 __device__ __noinline__ float exact_code(float x, float top, int root) {

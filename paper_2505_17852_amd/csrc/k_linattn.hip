@@ -51,13 +51,14 @@
 // segment from its own state.
 //
 // What bounds it. bf16, 16 sequences of 1,024 positions, 32 heads of 128: the forward pass moves its 0.54 GB in
-// 0.13 ms (4.2 TB/s, a large copy reaches 4.75); the backward pass reads nine tensors for the four it needs
-// (its three passes share most of that in L2) and takes 0.36 ms. There and on shorter or
-// fewer sequences (32 ragged ones of up to 777 positions, 16 heads of 64: 36 us, 2.3 TB/s; one of 8,192, 32 heads of
-// 128: 0.12 ms) it is a workgroup's chain per chunk - loads, LDS, four dependent products, two barriers - at the
-// two workgroups that fit a CU: without its matrix products the kernel takes 57% of its time, without
-// its loads 80%. fp32 is bound by the fp32 MFMAs (1/16 of the bf16 rate) of the wave with most score tiles: 64 sequences
-// of 256 positions, 4 heads of 64, forward and backward 87 us, 43 TFLOP/s of the recurrence's own operations.
+// 0.16 ms (3.4 TB/s, a large copy reaches 4.75); the backward pass reads nine tensors for the four it needs
+// (its three passes share most of that in L2) and takes 0.43 ms. There and on shorter or
+// fewer sequences (32 ragged ones of up to 777 positions, 16 heads of 64: 40 us, 2.1 TB/s; one of 8,192, 32 heads of
+// 128: 0.13 ms) it is a workgroup's chain per chunk - loads, LDS, four dependent products, two barriers (four with
+// slices of 128) - at the workgroups that fit a CU: two, by registers and LDS, three where states have 64 rows. The
+// matrix pipes are busy for a third of the cycles. fp32 waits in the same way, for the fp32 MFMAs (1/16 of the bf16 rate)
+// of the waves with most score tiles and at one or two workgroups a CU: 64 sequences of 256 positions, 4 heads of
+// 64, forward and backward 87 us, 43 TFLOP/s of the recurrence's own operations, the pipes busy for 36 and 49%.
 #include <hip/hip_runtime.h>
 
 #include "zo_layers.hpp"
@@ -706,8 +707,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DX == 64 && even ? 3 : 
 // Few positions: one after another, the state in registers (thread t: columns 4 (t % 16) .., rows t / 16 + 16 i of 64
 // columns), everything in fp32. A chunk of 64 would be mostly zeros, in a workgroup that takes a third of a CU or
 // all of it. All positions are read at once, and their outputs' sums joined at once.
-// Up to four positions: without states 0.04 to 0.09 ms for 256 sequences of 32 heads of 128 (bf16) against 0.12 in
-// chunks, fp32 0.04 to 0.10 against 0.25; eight positions take 0.17 against 0.12 (bf16).
+// One to four positions, 256 sequences of 32 heads of 128: without states 0.04 to 0.09 ms (bf16) against 0.15 in
+// chunks, fp32 0.04 to 0.10 against 0.34; with states 0.21 to 0.24 against 0.40, fp32 0.21 to 0.26 against 0.90.
+// Eight take 0.17 against 0.15 (bf16; fp32 0.18 against 0.34).
 constexpr int kFew = 4;         // positions
 constexpr int kFewPairs = 16;   // positions times y/z heads
 template <typename T, int ROWS, int PAIRS>
@@ -882,9 +884,8 @@ __global__ __launch_bounds__(kThreads) void linattn_scan_kernel(LinCall c, Plan 
 }
 
 // Segments of a call: enough workgroups for two on every CU, none shorter than four chunks; one where 256 workgroups
-// are there already (the states' pass over y and z costs more than the shorter chain saves: 512 workgroups, 32
-// sequences of 777, bf16, 16 heads on 4 states of 64: 39 us, in two segments 48; 16 sequences of 1,024, 32 heads of
-// 128: 137 and 176).
+// are there already (the states' pass over y and z costs more than the shorter chain saves: 512 workgroups, bf16, 32
+// sequences of 777, 16 heads on 4 states of 64: 49 us, in two segments 57; of 2,048, 16 heads of 64: 130 and 170).
 void split(int64_t workgroups, int T, int* segments, int* length) {
   int64_t s = workgroups >= 256 || workgroups == 0 ? 1 : (512 + workgroups - 1) / workgroups;
   const int64_t most = T / (4 * kChunk);
@@ -939,9 +940,8 @@ hipError_t launch(const LinCall& c, const Plan& pl, int dx, int slice, hipStream
 
 // Columns of z per workgroup: 128 where states have more than 64 rows and columns and no more
 // than 128 rows (x and y are then read once, and the scores formed once; 16 sequences of 1,024 positions, 32 heads
-// of 128, forward and backward: 0.49 ms against 0.54), 64 otherwise, where several query heads
-// add to one output, and where the states are too few to give every CU one (one sequence of 8,192
-// positions, 32 heads: 0.12 ms against 0.14).
+// of 128, forward and backward: 0.58 ms against 0.62), 64 otherwise, where several query heads
+// add to one output, and where the states are too few to give every CU one (half the workgroups would be left).
 int slice_of(int64_t states, int dk, int dv, int share, bool backward) {
   if ((backward ? states : states * share) < 256 || (backward && share > 1)) return 64;
   const int dx = backward ? std::max(dk, dv) : dk, dz = backward ? std::min(dk, dv) : dv;

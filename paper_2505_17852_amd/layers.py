@@ -196,7 +196,7 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_deca
     L = lib()
     B, T, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 4, scale)
     if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad
-                         or (initial_state is not None and initial_state.requires_grad)):
+                         or getattr(initial_state, "requires_grad", False)):
         _refuse_gradients()
     states = (B, Hkv, Dk, Dv)
     o, ho = _new_heads(q, B, T, Hq, Dv) if out is None else (out, _heads(out, "out", (B, T, Hq, Dv), q))
@@ -258,7 +258,8 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
         return _beside(stream, linear_attention_step, q, k, v, log_decay, state, scale, slots, out)
     L = lib()
     B, _, Hq, Hkv, Dk, Dv, s, hq, hk, hv = _sizes(q, k, v, 3, scale)
-    if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad or state.requires_grad):
+    if _recording() and (q.requires_grad or k.requires_grad or v.requires_grad
+                         or getattr(state, "requires_grad", False)):
         _refuse_gradients()
     n = state.shape[0]
     if n > 0x7fffffff:
@@ -361,7 +362,8 @@ class AdamW:
     """AdamW over a list of parameter tensors, all in one launch for up to 64 of them.
 
     params: contiguous device tensors, fp32 or bf16, updated in place, that share no memory (a tied tensor
-    is given once, with the sum of its gradients). weight_decay: one
+    is given once, with the sum of its gradients). bf16 values are rounded to nearest, which loses
+    changes under 2^-9 of them: where those count, keep fp32 parameters and cast them. weight_decay: one
     number, or one for each tensor. state_bits: 32 (m and v fp32) or 8 (m int8 and v uint8
     codes with m_scale and v_scale, the largest values of blocks of 256: see
     zo_layers.h). The moments of tensor i begin at offsets[i] of the flat m and v and take
@@ -423,7 +425,7 @@ class AdamW:
         """One step (asynchronous) with one contiguous fp32 or bf16 gradient for each tensor.
         grad_scale (device fp32 [1]) multiplies them; if it is not finite the step changes
         nothing, and skipped (device int32 [1]) is set to 1, else to 0. step_count goes up
-        either way."""
+        either way, and with it the bias corrections; who reads skipped may take the step off again."""
         grads = list(grads)
         if stream is not None:
             _beside(stream, self.step, grads, grad_scale, skipped)
