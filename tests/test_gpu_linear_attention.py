@@ -674,3 +674,27 @@ def test_states_are_as_exact_as_their_factors(layers, T, D, dtype):
     want = s["do"].astype(np.float64).transpose(0, 2, 1, 3) * np.exp(ld * (np.arange(T) + 1)[None, None, :, None])
     close("dinitial", got[:, :, :T], want, unit * np.abs(want) + 1e-37)
     assert not got[:, :, T:].any()
+
+
+def test_a_graph_captured_with_its_stream_named(layers):
+    """The capturing stream passed to each call: every replay, with eager work between, gives the eager result."""
+    s = make(np.random.default_rng(101), "bf16", 2, 300, 4, 2, 64, 64, True)
+    args = (s["q_d"], s["k_d"], s["v_d"], s["decay_d"])
+
+    def call(stream=None):
+        o, final = layers.linear_attention(*args, initial_state=s["initial_d"], return_state=True, stream=stream)
+        y, mean, rstd = layers.layer_norm(o, stream=stream)
+        return [o, final, y, *layers.linear_attention_backward(y, *args, initial_state=s["initial_d"], stream=stream)]
+
+    want = [t.clone() for t in call()]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call(torch.cuda.current_stream())
+    for _ in range(3):
+        for t in held:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(held, want))
+        assert all(torch.equal(x, y) for x, y in zip(call(), want))
